@@ -61,7 +61,9 @@ typedef enum {
     PSMC_E_TOO_LARGE = 8 /* problem needs more than the fixed scratch of psmc_logits_pass_static */
 } psmc_status;
 
-typedef enum { PSMC_F32 = 0, PSMC_BF16 = 1 } psmc_dtype;
+/* PSMC_F8 is for the pools of a paged cache only: codes of 8 bits (4 exponent bits, 3 mantissa bits) with one
+ * power-of-two scale per position and head (psmc_paged_kv below describes the layout). */
+typedef enum { PSMC_F32 = 0, PSMC_BF16 = 1, PSMC_F8 = 2 } psmc_dtype;
 
 /* Resampling schemes (Appendix E, "Resampling Choices": any unbiased scheme preserves the target). */
 typedef enum {
@@ -254,7 +256,8 @@ psmc_status psmc_kv_paged_append(psmc_ctx*, void* stream);
 /* At most 64 layers per call; pools 16-byte aligned with head_dim*sizeof(elem) a multiple of 16. */
 typedef struct {
     int n_layers;
-    void* const* k;      /* HOST array [n_layers] of DEVICE pointers, each pool [n_blocks, H, block_len, D] contiguous */
+    void* const* k;      /* HOST array [n_layers] of DEVICE pointers, each pool [n_blocks, H, block_len, D] contiguous;
+                          * PSMC_F8: [n_blocks, psmc_paged_block_bytes()] bytes                                        */
     void* const* v;
     int n_kv_heads;      /* H */
     int head_dim;        /* D */
@@ -273,6 +276,114 @@ psmc_status psmc_reindex_kv_paged(psmc_ctx*, const psmc_kv_pools* pools, void* s
 const int32_t* psmc_kv_paged_table(psmc_ctx*);      /* [R, max_blocks_per_row] */
 const int32_t* psmc_kv_paged_refcount(psmc_ctx*);   /* [n_blocks]              */
 const int32_t* psmc_kv_paged_free_count(psmc_ctx*); /* [1] blocks on the free list */
+
+/* ------------------------------------------------------------------------- */
+/* A language model's operators on the paged cache                             */
+/* ------------------------------------------------------------------------- */
+/* What the model's layers do with the cache between two psmc_step calls (the paper runs its model in another
+ * framework and describes only the cache's reorder): a layer's queries and keys get their rotary positions and the
+ * keys and values go into the cache (psmc_paged_write), every row's new token attends to the row's positions
+ * (psmc_paged_attend), and the cache can be had back as dense tensors (psmc_paged_read).  Each comes in a stateless
+ * form, which takes the table and the lengths as DEVICE arrays, and in a form on a context's own cache (psmc_kv_paged_*).
+ * None of them synchronises or allocates; all can be captured into a graph.
+ *
+ * Types: fp32 pools go with fp32 tensors, bf16 and 8-bit pools with bf16 tensors; sums are fp32.
+ * 8-bit pools: a block of one pool is psmc_paged_block_bytes() bytes: the codes [H, block_len, D] (1 sign, 4 exponent,
+ * 3 mantissa bits, bias 7; 0x7f is NaN, there is no infinity), then the scale bytes [H, block_len], then padding to 16
+ * bytes.  The value of a code is code * 2^(scale byte - 127).  When a position is written its scale is the smallest
+ * power of two that brings the head's largest finite component to at most 448, with the exponent kept within [-60, 60]
+ * (larger components saturate, smaller ones round to zero); components that are not finite become NaN.
+ *
+ * head_dim at most 256, and head_dim times the element size of the pool a multiple of 16 bytes; pools 16-byte aligned.
+ * A table entry that a call needs and that names no block (negative, or n_blocks and beyond), and a length beyond the
+ * table, raise PSMC_E_STATE in the status word: such positions are neither written nor read, the rest is done. */
+typedef struct {
+    void* k;              /* DEVICE pool of one layer's keys: [n_blocks, H, block_len, D], or the 8-bit blocks */
+    void* v;              /* the same for its values                                                         */
+    const int32_t* table; /* DEVICE [R, max_blocks], row stride table_ld: block of positions j*block_len ...   */
+    int64_t table_ld;
+    int R, n_blocks, block_len, max_blocks;
+    int n_kv_heads;       /* H */
+    int head_dim;         /* D */
+    psmc_dtype dt;
+} psmc_paged_kv;
+
+/* [n, heads, head_dim] on the DEVICE, unit stride along head_dim, the other strides in elements (so that queries, keys
+ * and values may be parts of one projection's output). */
+typedef struct {
+    void* data;
+    int64_t stride_row, stride_head;
+} psmc_heads;
+
+/* bytes of one block of one pool; 0 for bad arguments */
+size_t psmc_paged_block_bytes(int n_kv_heads, int block_len, int head_dim, psmc_dtype dt);
+
+/* Rotary positions.  Pair j of the first rot_dim components of a head turns by position * freqs[j]:
+ * (a, b) -> mscale * (a cos - b sin, b cos + a sin).  Pairs are components (j, j + rot_dim/2) or (2j, 2j + 1). */
+typedef enum { PSMC_ROPE_HALF = 0, PSMC_ROPE_PAIRS = 1 } psmc_rope_layout;
+typedef struct {
+    const double* freqs;   /* DEVICE [rot_dim / 2]: radians per position */
+    int rot_dim;           /* even, 2 .. head_dim */
+    psmc_rope_layout layout;
+    double mscale;         /* factor on cosine and sine (1 = none) */
+} psmc_rope;
+
+/* Fills a HOST array [rot_dim / 2] with frequencies theta^(-2j/rot_dim), scaled for contexts `factor` times as long as
+ * the trained_len positions a model was trained on:
+ *   PSMC_ROPE_PLAIN   unscaled                         PSMC_ROPE_LINEAR  all divided by factor
+ *   PSMC_ROPE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) instead of theta (rot_dim >= 4)
+ *   PSMC_ROPE_BANDS   a pair that makes more than `high` turns over trained_len positions keeps its frequency, one that
+ *                     makes fewer than `low` has it divided, between them the two are mixed linearly in the turns
+ *   PSMC_ROPE_YARN    the same with the mixture linear in j, between the pairs that make `high` and `low` turns, and
+ *                     mscale = 0.1 ln(factor) + 1 (1 for all others)
+ * low < high and trained_len are read by the last two only.  theta > 1, factor >= 1.  Host only. */
+typedef enum { PSMC_ROPE_PLAIN = 0, PSMC_ROPE_LINEAR = 1, PSMC_ROPE_BASE = 2, PSMC_ROPE_BANDS = 3, PSMC_ROPE_YARN = 4 } psmc_rope_scaling;
+psmc_status psmc_rope_frequencies(psmc_rope_scaling kind, int rot_dim, double theta, double factor, double low, double high,
+                                  int trained_len, double* freqs_out, double* mscale_out);
+
+/* n tokens: token i is position positions[i] of row rows[i] (both DEVICE; rows NULL: row i, n <= R).  Its keys k [n, H, D]
+ * get their rotary positions (rope NULL: none) and go into the cache with its values v; its queries q [n, Hq, D], when
+ * given, get theirs into q_out, which may be q itself.  Angles are formed in 64 bits.  Tokens with rows[i] < 0 are padding, and
+ * tokens of rows with skip[row] != 0 (DEVICE [R], may be NULL) are left out: nothing of theirs is read or written.
+ * The block of a position must belong to the row alone or be written by one of its owners only; a position that appears
+ * twice in a call gets one of the two tokens. */
+psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows, const int32_t* positions,
+                             const uint8_t* skip, const psmc_rope* rope, const psmc_heads* k, const psmc_heads* v,
+                             int n_q_heads, const psmc_heads* q, const psmc_heads* q_out, int32_t* status_word, void* stream);
+
+/* out[r, h] = sum_p softmax_p(scale * q[r, h] . k_p) v_p over the positions p < lens[r] + extra of row r, for query heads
+ * h = 0 .. Hq-1 (a multiple of H: head h reads key-value head h / (Hq / H)).  lse (DEVICE [R, Hq] fp32, may be NULL)
+ * receives ln sum_p exp(scale * q . k_p), so that results over parts of a context can be joined.  A row without
+ * positions gets zeros and lse = -inf; rows with skip[r] != 0 are left as they were.  Blocks that several rows share are
+ * read once for all of them where they lie within a run of 32 rows.  scratch: psmc_paged_attend_scratch_bytes() bytes,
+ * 256-byte aligned, contents irrelevant; calls that may overlap (other streams, graphs replayed side by side) need
+ * scratch of their own.  out may not overlap q. */
+size_t psmc_paged_attend_scratch_bytes(int R, int n_q_heads, int n_kv_heads, int head_dim);
+psmc_status psmc_paged_attend(const psmc_paged_kv* kv, const int32_t* lens, int extra, const uint8_t* skip, int n_q_heads,
+                              const psmc_heads* q, const psmc_heads* out, float scale, float* lse, void* scratch,
+                              size_t scratch_bytes, int32_t* status_word, void* stream);
+
+/* Positions 0 .. lens[r] of every row into dense tensors [R, H, max_len, D] ((position, dim) contiguous, the layout of
+ * psmc_kv_desc; bf16 for 8-bit pools, exact); other positions and rows with skip[r] != 0 are left as they were.  k_out or
+ * v_out may be NULL.  lens[r] > max_len raises PSMC_E_STATE and is cut. */
+psmc_status psmc_paged_read(const psmc_paged_kv* kv, const int32_t* lens, const uint8_t* skip, void* k_out, void* v_out,
+                            int max_len, int64_t stride_row, int64_t stride_head, int32_t* status_word, void* stream);
+
+/* The same on layer `layer` of a context's paged cache (psmc_kv_paged_create).
+ *   write   rows and positions NULL, n = R: the next token of every live row, at position len[r] (before psmc_step
+ *           counts it); finished rows are left out.  Else the given positions, e.g. the prompts: a block that
+ *           psmc_kv_paged_create shared within a group is written through one of its rows.
+ *   attend  every live row attends to its len[r] positions and the new one, len[r] + 1 in all.
+ *   read    len[r] positions of every row, finished rows too.
+ * Device-side errors go to the context's status word. */
+psmc_status psmc_kv_paged_write(psmc_ctx*, const psmc_kv_pools* pools, int layer, int n, const int32_t* rows,
+                                const int32_t* positions, const psmc_rope* rope, const psmc_heads* k, const psmc_heads* v,
+                                int n_q_heads, const psmc_heads* q, const psmc_heads* q_out, void* stream);
+psmc_status psmc_kv_paged_attend(psmc_ctx*, const psmc_kv_pools* pools, int layer, int n_q_heads, const psmc_heads* q,
+                                 const psmc_heads* out, float scale, float* lse, void* scratch, size_t scratch_bytes,
+                                 void* stream);
+psmc_status psmc_kv_paged_read(psmc_ctx*, const psmc_kv_pools* pools, int layer, void* k_out, void* v_out, int max_len,
+                               int64_t stride_row, int64_t stride_head, void* stream);
 
 /* ------------------------------------------------------------------------- */
 /* Output (last step of Algorithm 1)                                          */

@@ -7,6 +7,7 @@ and the stream: tensors are passed as ``data_ptr()``, the stream as ``cuda_strea
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -17,7 +18,10 @@ from . import build as _build
 
 OK, E_INVAL, E_NOMEM, E_CUDA, E_STATE, E_NUMERIC, E_TIMEOUT, E_HAZARD, E_TOO_LARGE = range(9)
 STATIC_SCRATCH_BYTES = 4 << 20
-F32, BF16 = 0, 1
+F32, BF16, F8 = 0, 1, 2
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "yarn": 4}
+ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+MAX_HEAD_DIM = 256
 SYSTEMATIC, STRATIFIED, MULTINOMIAL, RESIDUAL = 0, 1, 2, 3
 
 _lib = None
@@ -39,6 +43,20 @@ class KvDesc(C.Structure):
 class KvPools(C.Structure):
     _fields_ = [("n_layers", C.c_int), ("k", C.POINTER(C.c_void_p)), ("v", C.POINTER(C.c_void_p)),
                 ("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("dt", C.c_int)]
+
+
+class PagedKvDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("table_ld", C.c_int64), ("R", C.c_int),
+                ("n_blocks", C.c_int), ("block_len", C.c_int), ("max_blocks", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("dt", C.c_int)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("rot_dim", C.c_int), ("layout", C.c_int), ("mscale", C.c_double)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
 
 
 def lib():
@@ -107,6 +125,25 @@ def lib():
         for name in ("psmc_kv_paged_table", "psmc_kv_paged_refcount", "psmc_kv_paged_free_count"):
             getattr(L, name).restype = C.c_void_p
             getattr(L, name).argtypes = [vp]
+        hp, ip = C.POINTER(Heads), C.c_int
+        L.psmc_paged_block_bytes.restype = C.c_size_t
+        L.psmc_paged_block_bytes.argtypes = [ip, ip, ip, ip]
+        L.psmc_rope_frequencies.restype = ip
+        L.psmc_rope_frequencies.argtypes = [ip, ip, C.c_double, C.c_double, C.c_double, C.c_double, ip, vp, vp]
+        L.psmc_paged_write.restype = ip
+        L.psmc_paged_write.argtypes = [C.POINTER(PagedKvDesc), ip, vp, vp, vp, C.POINTER(RopeDesc), hp, hp, ip, hp, hp, vp, vp]
+        L.psmc_paged_attend_scratch_bytes.restype = C.c_size_t
+        L.psmc_paged_attend_scratch_bytes.argtypes = [ip, ip, ip, ip]
+        L.psmc_paged_attend.restype = ip
+        L.psmc_paged_attend.argtypes = [C.POINTER(PagedKvDesc), vp, ip, vp, ip, hp, hp, C.c_float, vp, vp, C.c_size_t, vp, vp]
+        L.psmc_paged_read.restype = ip
+        L.psmc_paged_read.argtypes = [C.POINTER(PagedKvDesc), vp, vp, vp, vp, ip, C.c_int64, C.c_int64, vp, vp]
+        L.psmc_kv_paged_write.restype = ip
+        L.psmc_kv_paged_write.argtypes = [vp, C.POINTER(KvPools), ip, ip, vp, vp, C.POINTER(RopeDesc), hp, hp, ip, hp, hp, vp]
+        L.psmc_kv_paged_attend.restype = ip
+        L.psmc_kv_paged_attend.argtypes = [vp, C.POINTER(KvPools), ip, ip, hp, hp, C.c_float, vp, vp, C.c_size_t, vp]
+        L.psmc_kv_paged_read.restype = ip
+        L.psmc_kv_paged_read.argtypes = [vp, C.POINTER(KvPools), ip, vp, vp, ip, C.c_int64, C.c_int64, vp]
         L.psmc_shard_sweep.restype = C.c_int
         L.psmc_shard_sweep.argtypes = [vp, vp, C.c_int, C.c_int64, C.c_int, vp, vp]
         L.psmc_shard_locate.restype = C.c_int
@@ -329,6 +366,7 @@ class Psmc:
     def make_kv_pools(self, k_pools, v_pools):
         """k_pools / v_pools: lists (one per layer) of contiguous CUDA tensors [n_blocks, H, block_len, D]."""
         p0 = k_pools[0]
+        assert p0.dtype != torch.uint8, "8-bit pools carry no shape: make_kv_pools_f8"
         nb, H, Bl, D = p0.shape
         assert (nb, Bl) == self._paged[:2]
         n = len(k_pools)
@@ -339,6 +377,60 @@ class Psmc:
         d = KvPools(n, C.cast(ka, C.POINTER(C.c_void_p)), C.cast(va, C.POINTER(C.c_void_p)), H, D, _dtype_code(p0))
         d._keep = (ka, va, list(k_pools), list(v_pools))
         return d
+
+    def make_kv_pools_f8(self, k_pools, v_pools, n_kv_heads: int, head_dim: int):
+        """k_pools / v_pools: lists of contiguous CUDA uint8 tensors [n_blocks, paged_block_bytes(...)] (8-bit codes and scales)."""
+        n = len(k_pools)
+        nbytes = paged_block_bytes(n_kv_heads, self._paged[1], head_dim, F8)
+        for t in list(k_pools) + list(v_pools):
+            assert t.shape == (self._paged[0], nbytes) and t.is_contiguous() and t.dtype == torch.uint8 and t.is_cuda
+        ka = (C.c_void_p * n)(*[t.data_ptr() for t in k_pools])
+        va = (C.c_void_p * n)(*[t.data_ptr() for t in v_pools])
+        d = KvPools(n, C.cast(ka, C.POINTER(C.c_void_p)), C.cast(va, C.POINTER(C.c_void_p)), n_kv_heads, head_dim, F8)
+        d._keep = (ka, va, list(k_pools), list(v_pools))
+        return d
+
+    # ---- a language model's operators on the context's paged cache
+    def kv_paged_write(self, pools: KvPools, layer: int, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor = None,
+                       q_out: torch.Tensor = None, rope: "Rope" = None, rows: torch.Tensor = None,
+                       positions: torch.Tensor = None, stream=None):
+        """psmc_kv_paged_write: the next token of every live row (k, v [R, H, D], q [R, Hq, D]), or with rows and positions
+        (int32 [n]) any tokens.  Returns q_out (q with its rotary positions), allocated if not given."""
+        n = k.shape[0]
+        io = _check_kv_tokens(pools.dt, pools.n_kv_heads, pools.head_dim, n, k, v)
+        if rows is None:
+            assert positions is None and n == self.R
+        else:
+            _check_ints(rows, n, k.device)
+            _check_ints(positions, n, k.device)
+        q_out = _check_queries(q, q_out, n, pools.head_dim, io, k.device, stream)
+        _on_device(k.device, lambda: _check(lib().psmc_kv_paged_write(
+            self._h, C.byref(pools), layer, n, _ptr(rows), _ptr(positions), _ref(rope), _heads(k), _heads(v),
+            0 if q is None else q.shape[1], _heads(q), _heads(q_out), _stream(stream)), "psmc_kv_paged_write"))
+        return q_out
+
+    def kv_paged_attend(self, pools: KvPools, layer: int, q: torch.Tensor, scale: float, out: torch.Tensor = None,
+                        lse: torch.Tensor = None, scratch: torch.Tensor = None, stream=None):
+        """psmc_kv_paged_attend: q [R, Hq, D] of every row's new token over its len + 1 positions (finished rows of out and
+        lse are left as they were; zeros in an out allocated here)."""
+        io = _check_queries_shape(q, self.R, pools.n_kv_heads, pools.head_dim, pools.dt)
+        if out is None:
+            with _allocate_on(stream):
+                out = torch.zeros_like(q)
+        _check_out(q, out, io)
+        _check_lse(lse, q)
+        scratch = _attend_scratch(scratch, self.R, q.shape[1], pools.n_kv_heads, pools.head_dim, q.device, stream)
+        _on_device(q.device, lambda: _check(lib().psmc_kv_paged_attend(
+            self._h, C.byref(pools), layer, q.shape[1], _heads(q), _heads(out), scale, _ptr(lse), scratch.data_ptr(),
+            scratch.numel(), _stream(stream)), "psmc_kv_paged_attend"))
+        return out
+
+    def kv_paged_read(self, pools: KvPools, layer: int, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
+        """psmc_kv_paged_read: the live positions of every row into dense [R, H, max_len, D] tensors."""
+        d = _check_dense(k_out, v_out, self.R, pools.n_kv_heads, pools.head_dim, pools.dt)
+        _on_device(d.device, lambda: _check(lib().psmc_kv_paged_read(
+            self._h, C.byref(pools), layer, _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0), d.stride(1),
+            _stream(stream)), "psmc_kv_paged_read"))
 
     def reindex_kv_paged(self, pools: KvPools, stream=None):
         _check(lib().psmc_reindex_kv_paged(self._h, C.byref(pools), _stream(stream)), "psmc_reindex_kv_paged")
@@ -421,6 +513,203 @@ def init(N, V, alpha, tau, ess_thresh, ramp, seed, eos_id) -> Psmc:
 def init_batched(G, N, V, alpha, tau, ess_thresh, ramp, seed, eos_id, T_max, prompt_len=None) -> Psmc:
     """psmc_init_batched: G independent groups."""
     return Psmc(N, V, alpha, tau, ess_thresh, ramp, seed, eos_id, G=G, T_max=T_max, prompt_len=prompt_len)
+
+
+# ---------------------------------------------------------------- a language model's operators on a paged cache
+def paged_block_bytes(n_kv_heads: int, block_len: int, head_dim: int, dtype_code: int) -> int:
+    """psmc_paged_block_bytes: bytes of one block of one pool (F32, BF16, F8)."""
+    return lib().psmc_paged_block_bytes(n_kv_heads, block_len, head_dim, dtype_code)
+
+
+def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                     high: float = 4.0, trained_len: int = 8192):
+    """psmc_rope_frequencies: (float64 numpy [rot_dim / 2], mscale); scaling: none, linear, base, bands or yarn."""
+    out, m = np.empty(max(rot_dim // 2, 1), np.float64), C.c_double()
+    _check(lib().psmc_rope_frequencies(ROPE_SCALINGS[scaling], rot_dim, theta, factor, low, high, trained_len,
+                                       out.ctypes.data, C.byref(m)), "psmc_rope_frequencies")
+    return out, m.value
+
+
+class Rope(RopeDesc):
+    """psmc_rope over a CUDA float64 tensor of frequencies [rot_dim / 2]; layout: half or pairs."""
+
+    def __init__(self, freqs: torch.Tensor, layout: str = "half", mscale: float = 1.0):
+        assert freqs.is_cuda and freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous()
+        super().__init__(freqs.data_ptr(), 2 * freqs.numel(), ROPE_LAYOUTS[layout], mscale)
+        self._keep = freqs
+
+
+class PagedKv(PagedKvDesc):
+    """psmc_paged_kv: one layer of a paged cache, as the stateless operators take it.
+
+    k, v: contiguous CUDA pools [n_blocks, H, block_len, D] (float32 or bfloat16), or uint8 [n_blocks,
+    paged_block_bytes(...)] (8-bit).  table: CUDA int32 [R, max_blocks], unit stride along the blocks."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_kv_heads: int, head_dim: int, block_len: int):
+        dt = F8 if k.dtype == torch.uint8 else _dtype_code(k)
+        shape = (paged_block_bytes(n_kv_heads, block_len, head_dim, F8),) if dt == F8 else (n_kv_heads, block_len, head_dim)
+        for t in (k, v):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == k.dtype and t.shape == (k.shape[0],) + shape
+            assert t.device == k.device
+        assert table.device == k.device and table.dtype == torch.int32 and table.dim() == 2 and table.stride(1) == 1
+        super().__init__(k.data_ptr(), v.data_ptr(), table.data_ptr(), table.stride(0), table.shape[0], k.shape[0], block_len,
+                         table.shape[1], n_kv_heads, head_dim, dt)
+        self._keep = (k, v, table)
+        self.device = k.device
+
+
+def _on_device(device, call):
+    """Launches belong to the device of their tensors, whichever is current."""
+    if device.index == torch.cuda.current_device():
+        return call()
+    with torch.cuda.device(device):
+        return call()
+
+
+def _allocate_on(stream):
+    """What a call allocates belongs to the stream it launches on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+def _ref(desc):
+    return None if desc is None else C.byref(desc)
+
+
+def _heads(t):
+    return None if t is None else C.byref(Heads(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+def _io_dtype(dtype_code: int):
+    return torch.float32 if dtype_code == F32 else torch.bfloat16
+
+
+def _check_kv_tokens(dtype_code, H, D, n, k, v):
+    io = _io_dtype(dtype_code)
+    for t in (k, v):
+        assert t.is_cuda and t.dtype == io and t.shape == (n, H, D) and t.stride(2) == 1 and t.device == k.device
+    return io
+
+
+def _check_queries(q, q_out, n, D, io, device, stream):
+    if q is None:
+        assert q_out is None
+        return None
+    if q_out is None:
+        with _allocate_on(stream):
+            q_out = torch.empty_like(q)
+    for t in (q, q_out):
+        assert t.device == device and t.dtype == io and t.dim() == 3 and t.shape == q.shape and t.stride(2) == 1
+    assert q.shape[0] == n and q.shape[2] == D
+    return q_out
+
+
+def _check_queries_shape(q, R, H, D, dtype_code):
+    io = _io_dtype(dtype_code)
+    assert q.is_cuda and q.dtype == io and q.dim() == 3 and q.stride(2) == 1
+    assert q.shape[0] == R and q.shape[2] == D and q.shape[1] % H == 0
+    return io
+
+
+def _check_out(q, out, io):
+    assert out.device == q.device and out.dtype == io and out.shape == q.shape and out.stride(2) == 1
+
+
+def _check_lse(lse, q):
+    if lse is not None:
+        assert lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
+
+
+def _check_ints(t, n, device):
+    assert t is not None and t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n
+
+
+def _check_skip(skip, R, device):
+    if skip is not None:
+        assert skip.device == device and skip.dtype == torch.uint8 and skip.is_contiguous() and skip.numel() == R
+
+
+def _check_word(word, device):
+    if word is not None:
+        assert word.device == device and word.dtype == torch.int32 and word.numel() >= 1
+
+
+def _check_dense(k_out, v_out, R, H, D, dtype_code):
+    d = k_out if k_out is not None else v_out
+    for t in (k_out, v_out):
+        if t is not None:
+            assert t.is_cuda and t.dtype == _io_dtype(dtype_code) and t.dim() == 4 and t.device == d.device
+            assert t.shape == d.shape and t.stride() == d.stride()
+    assert d.shape[0] == R and d.shape[1] == H and d.shape[3] == D and d.stride(3) == 1 and d.stride(2) == D
+    return d
+
+
+def _attend_scratch(scratch, R, Hq, H, D, device, stream):
+    """Workspace of one call: the caller's, or a fresh one (from the graph's own pool while one is captured)."""
+    need = lib().psmc_paged_attend_scratch_bytes(R, Hq, H, D)
+    if scratch is None:
+        with _allocate_on(stream):
+            scratch = torch.empty(need, dtype=torch.uint8, device=device)
+    assert scratch.device == device and scratch.dtype == torch.uint8 and scratch.is_contiguous() and scratch.numel() >= need
+    return scratch
+
+
+def paged_write(cache: PagedKv, k: torch.Tensor, v: torch.Tensor, rows, positions: torch.Tensor, q: torch.Tensor = None,
+                q_out: torch.Tensor = None, rope: Rope = None, skip: torch.Tensor = None, status_word: torch.Tensor = None,
+                stream=None):
+    """psmc_paged_write: k, v [n, H, D] (and q [n, Hq, D]) of tokens at positions[i] of rows[i] (int32; rows None: row i).
+    Returns q_out (q with its rotary positions), allocated if not given."""
+    n, dev = k.shape[0], cache.device
+    io = _check_kv_tokens(cache.dt, cache.n_kv_heads, cache.head_dim, n, k, v)
+    assert k.device == dev
+    if rows is not None:
+        _check_ints(rows, n, dev)
+    _check_ints(positions, n, dev)
+    _check_skip(skip, cache.R, dev)
+    _check_word(status_word, dev)
+    q_out = _check_queries(q, q_out, n, cache.head_dim, io, dev, stream)
+    _on_device(dev, lambda: _check(lib().psmc_paged_write(
+        C.byref(cache), n, _ptr(rows), positions.data_ptr(), _ptr(skip), _ref(rope), _heads(k), _heads(v),
+        0 if q is None else q.shape[1], _heads(q), _heads(q_out), _ptr(status_word), _stream(stream)), "psmc_paged_write"))
+    return q_out
+
+
+def paged_attend(cache: PagedKv, q: torch.Tensor, lens: torch.Tensor, scale: float, out: torch.Tensor = None,
+                 lse: torch.Tensor = None, skip: torch.Tensor = None, extra: int = 0, scratch: torch.Tensor = None,
+                 status_word: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """psmc_paged_attend: q [R, Hq, D], one token per row, over positions 0 .. lens[r] + extra of the row (lens int32 [R]).
+    lse: float32 [R, Hq] or None.  Rows with skip != 0 are left as they were (zeros in an out allocated here)."""
+    dev = cache.device
+    io = _check_queries_shape(q, cache.R, cache.n_kv_heads, cache.head_dim, cache.dt)
+    assert q.device == dev
+    _check_ints(lens, cache.R, dev)
+    _check_skip(skip, cache.R, dev)
+    _check_word(status_word, dev)
+    _check_lse(lse, q)
+    if out is None:
+        with _allocate_on(stream):
+            out = torch.empty_like(q) if skip is None else torch.zeros_like(q)
+    _check_out(q, out, io)
+    scratch = _attend_scratch(scratch, cache.R, q.shape[1], cache.n_kv_heads, cache.head_dim, dev, stream)
+    _on_device(dev, lambda: _check(lib().psmc_paged_attend(
+        C.byref(cache), lens.data_ptr(), extra, _ptr(skip), q.shape[1], _heads(q), _heads(out), scale, _ptr(lse),
+        scratch.data_ptr(), scratch.numel(), _ptr(status_word), _stream(stream)), "psmc_paged_attend"))
+    return out
+
+
+def paged_read(cache: PagedKv, lens: torch.Tensor, k_out: torch.Tensor = None, v_out: torch.Tensor = None,
+               skip: torch.Tensor = None, status_word: torch.Tensor = None, stream=None) -> None:
+    """psmc_paged_read: positions 0 .. lens[r] of every row into dense [R, H, max_len, D] tensors (one of them may be None)."""
+    dev = cache.device
+    d = _check_dense(k_out, v_out, cache.R, cache.n_kv_heads, cache.head_dim, cache.dt)
+    assert d.device == dev
+    _check_ints(lens, cache.R, dev)
+    _check_skip(skip, cache.R, dev)
+    _check_word(status_word, dev)
+    _on_device(dev, lambda: _check(lib().psmc_paged_read(
+        C.byref(cache), lens.data_ptr(), _ptr(skip), _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0), d.stride(1),
+        _ptr(status_word), _stream(stream)), "psmc_paged_read"))
 
 
 def logits_pass_scratch_bytes(R: int, V: int) -> int:

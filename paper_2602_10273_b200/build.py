@@ -18,7 +18,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]
 
 PRODUCT_SOURCES = ["context.cu", "logits_pass.cu", "step_fused.cu", "weights_resample.cu", "vocab_shard.cu",
-                   "masked_proposal.cu", "reindex_kv.cu", "paged_kv.cu", "select.cu"]
+                   "masked_proposal.cu", "reindex_kv.cu", "paged_kv.cu",
+                   "paged_write.cu", "paged_attend.cu", "paged_read.cu", "select.cu"]
 WORKLOAD_SOURCES = ["workload.cu"]
 
 

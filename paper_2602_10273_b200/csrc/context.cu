@@ -5,6 +5,7 @@
 #include <mutex>
 #include <new>
 #include <utility>
+#include <math.h>
 #include <string.h>
 #include <vector>
 
@@ -614,6 +615,212 @@ extern "C" psmc_status psmc_reindex_kv(psmc_ctx* c, const psmc_kv_desc* src, con
     return PSMC_OK;
 }
 
+namespace {
+
+int pool_elem_bytes(int dt) { return dt == PSMC_F32 ? 4 : (dt == PSMC_BF16 ? 2 : 1); }
+
+// One layer of a paged cache: the checks every operator on it makes.
+psmc_status view_of(const psmc_paged_kv* kv, PagedView* out) {
+    if (!kv || !kv->k || !kv->v || !kv->table || kv->R < 1 || kv->n_blocks < 1 || kv->block_len < 1 || kv->max_blocks < 1 ||
+        kv->table_ld < kv->max_blocks || kv->n_kv_heads < 1 || kv->head_dim < 1 || kv->head_dim > kMaxHeadDim)
+        return PSMC_E_INVAL;
+    if (kv->dt != PSMC_F32 && kv->dt != PSMC_BF16 && kv->dt != PSMC_F8) return PSMC_E_INVAL;
+    const int elem = pool_elem_bytes(kv->dt);
+    if (((uint64_t)(uintptr_t)kv->k | (uint64_t)(uintptr_t)kv->v | (uint64_t)(kv->head_dim * elem)) % 16 != 0) return PSMC_E_INVAL;
+    if ((uint64_t)(uintptr_t)kv->table % 4 != 0) return PSMC_E_INVAL;
+    // positions, and the elements of one block, are counted in an int
+    if ((int64_t)kv->max_blocks * kv->block_len >= ((int64_t)1 << 31) ||
+        (int64_t)kv->n_kv_heads * kv->block_len >= ((int64_t)1 << 31) / kv->head_dim / elem)
+        return PSMC_E_INVAL;
+    PagedView& c = *out;
+    c.k = static_cast<char*>(kv->k); c.v = static_cast<char*>(kv->v);
+    c.table = kv->table; c.table_ld = kv->table_ld;
+    c.R = kv->R; c.n_blocks = kv->n_blocks; c.block_len = kv->block_len; c.max_blocks = kv->max_blocks;
+    c.H = kv->n_kv_heads; c.D = kv->head_dim; c.dt = kv->dt;
+    c.scale_at = (int64_t)kv->n_kv_heads * kv->block_len * kv->head_dim * elem;
+    c.blk_bytes = c.scale_at + (kv->dt == PSMC_F8 ? paged_scale_bytes(kv->n_kv_heads, kv->block_len) : 0);
+    return PSMC_OK;
+}
+
+// layer `layer` of the context's own cache, as the stateless calls take it
+psmc_status layer_of(const psmc_ctx* c, const psmc_kv_pools* pools, int layer, psmc_paged_kv* kv) {
+    if (!c || !pools || !pools->k || !pools->v || layer < 0 || layer >= pools->n_layers) return PSMC_E_INVAL;
+    if (!c->paged.table) return PSMC_E_STATE;
+    *kv = psmc_paged_kv{pools->k[layer], pools->v[layer], c->paged.table, c->paged.max_blocks, c->R, c->paged.n_blocks,
+                        c->paged.block_len, c->paged.max_blocks, pools->n_kv_heads, pools->head_dim, pools->dt};
+    return PSMC_OK;
+}
+
+// heads of `n` rows: element alignment, and strides that an address can follow
+bool heads_ok(const psmc_heads* h, int dt) {
+    return h && h->data && (uint64_t)(uintptr_t)h->data % (dt == PSMC_F32 ? 4 : 2) == 0;
+}
+HeadsView heads_view(const psmc_heads* h) { return HeadsView{h->data, h->stride_row, h->stride_head}; }
+
+psmc_status paged_write(const PagedView& c, int n, const int32_t* rows, const int32_t* positions, const uint8_t* skip,
+                        const psmc_rope* rope, const psmc_heads* k, const psmc_heads* v, int Hq, const psmc_heads* q,
+                        const psmc_heads* q_out, int32_t* status, cudaStream_t s) {
+    if (n == 0) return PSMC_OK;  // an empty tensor has no address either
+    if (n < 0 || !positions || !heads_ok(k, c.dt) || !heads_ok(v, c.dt)) return PSMC_E_INVAL;
+    if ((q == nullptr) != (q_out == nullptr)) return PSMC_E_INVAL;
+    if (q && (Hq < 1 || !heads_ok(q, c.dt) || !heads_ok(q_out, c.dt))) return PSMC_E_INVAL;
+    if (!rows && n > c.R) return PSMC_E_INVAL;
+    PagedWrite w{};
+    w.n = n; w.rows = rows; w.positions = positions; w.skip = skip; w.status = status;
+    w.k_in = heads_view(k); w.v_in = heads_view(v);
+    if (q) {
+        w.q = true; w.Hq = Hq; w.q_in = heads_view(q); w.q_out = heads_view(q_out);
+    }
+    w.mscale = 1.f;
+    if (rope) {
+        if (!rope->freqs || rope->rot_dim < 2 || rope->rot_dim % 2 != 0 || rope->rot_dim > c.D ||
+            (rope->layout != PSMC_ROPE_HALF && rope->layout != PSMC_ROPE_PAIRS))
+            return PSMC_E_INVAL;
+        w.freqs = rope->freqs; w.rot = rope->rot_dim; w.pairs = rope->layout == PSMC_ROPE_PAIRS; w.mscale = (float)rope->mscale;
+    }
+    return launch_paged_write(c, w, s) == cudaSuccess ? PSMC_OK : PSMC_E_CUDA;
+}
+
+psmc_status paged_attend(const PagedView& c, const int32_t* lens, int extra, const uint8_t* skip, int Hq, const psmc_heads* q,
+                         const psmc_heads* out, float scale, float* lse, void* scratch, size_t scratch_bytes, int32_t* status,
+                         cudaStream_t s) {
+    if (!lens || extra < 0 || Hq < 1 || Hq % c.H != 0 || !heads_ok(q, c.dt) || !heads_ok(out, c.dt)) return PSMC_E_INVAL;
+    if (!scratch || (uint64_t)(uintptr_t)scratch % 256 != 0 || scratch_bytes < psmc_paged_attend_scratch_bytes(c.R, Hq, c.H, c.D))
+        return PSMC_E_INVAL;
+    PagedAttend a{};
+    a.lens = lens; a.extra = extra; a.skip = skip; a.Hq = Hq; a.q = heads_view(q); a.out = heads_view(out); a.scale = scale;
+    a.lse = lse; a.scratch = scratch; a.status = status;
+    return launch_paged_attend(c, a, s) == cudaSuccess ? PSMC_OK : PSMC_E_CUDA;
+}
+
+psmc_status paged_read(const PagedView& c, const int32_t* lens, const uint8_t* skip, void* k_out, void* v_out, int max_len,
+                       int64_t stride_row, int64_t stride_head, int32_t* status, cudaStream_t s) {
+    if (!lens || (!k_out && !v_out) || max_len < 1 || stride_head < (int64_t)max_len * c.D ||
+        stride_row < (int64_t)c.H * stride_head)
+        return PSMC_E_INVAL;
+    if (((uint64_t)(uintptr_t)k_out | (uint64_t)(uintptr_t)v_out) % (c.dt == PSMC_F32 ? 4 : 2) != 0) return PSMC_E_INVAL;
+    PagedRead a{};
+    a.lens = lens; a.skip = skip; a.k = k_out; a.v = v_out; a.max_len = max_len; a.stride_row = stride_row;
+    a.stride_head = stride_head; a.status = status;
+    return launch_paged_read(c, a, s) == cudaSuccess ? PSMC_OK : PSMC_E_CUDA;
+}
+
+}  // namespace
+
+extern "C" size_t psmc_paged_block_bytes(int n_kv_heads, int block_len, int head_dim, psmc_dtype dt) {
+    if (n_kv_heads < 1 || block_len < 1 || head_dim < 1 || (dt != PSMC_F32 && dt != PSMC_BF16 && dt != PSMC_F8)) return 0;
+    return (size_t)n_kv_heads * block_len * head_dim * pool_elem_bytes(dt) +
+           (dt == PSMC_F8 ? (size_t)paged_scale_bytes(n_kv_heads, block_len) : 0);
+}
+
+extern "C" psmc_status psmc_rope_frequencies(psmc_rope_scaling kind, int rot_dim, double theta, double factor, double low,
+                                             double high, int trained_len, double* freqs_out, double* mscale_out) {
+    const double pi = 3.14159265358979323846;
+    if (!freqs_out || rot_dim < 2 || rot_dim % 2 != 0 || !(theta > 1.0) || !(factor >= 1.0)) return PSMC_E_INVAL;
+    if ((int)kind < 0 || (int)kind > 4) return PSMC_E_INVAL;
+    const bool by_turns = kind == PSMC_ROPE_BANDS || kind == PSMC_ROPE_YARN;
+    if (by_turns && (!(low > 0.0) || !(high > low) || trained_len < 1)) return PSMC_E_INVAL;
+    if (kind == PSMC_ROPE_BASE) {
+        if (rot_dim < 4) return PSMC_E_INVAL;
+        theta *= pow(factor, (double)rot_dim / (rot_dim - 2));
+    }
+    // the pair (as a real number) that makes `turns` whole turns over trained_len positions
+    const auto pair_of = [&](double turns) { return rot_dim * log(trained_len / (2 * pi * turns)) / (2 * log(theta)); };
+    double first = 0.0, last = 0.0;
+    if (kind == PSMC_ROPE_YARN) {
+        first = floor(pair_of(high)); last = ceil(pair_of(low));
+        if (first < 0.0) first = 0.0;
+        if (last > rot_dim - 1) last = rot_dim - 1;
+    }
+    for (int j = 0; j < rot_dim / 2; ++j) {
+        double f = pow(theta, -2.0 * j / rot_dim), keep = 1.0;  // keep: share of the unscaled frequency
+        if (kind == PSMC_ROPE_LINEAR) keep = 0.0;
+        if (kind == PSMC_ROPE_BANDS) keep = (trained_len * f / (2 * pi) - low) / (high - low);
+        if (kind == PSMC_ROPE_YARN) keep = 1.0 - (j - first) / (last > first ? last - first : 0.001);
+        keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+        freqs_out[j] = f * keep + f / factor * (1.0 - keep);
+    }
+    if (mscale_out) *mscale_out = kind == PSMC_ROPE_YARN ? 0.1 * log(factor) + 1.0 : 1.0;
+    return PSMC_OK;
+}
+
+extern "C" size_t psmc_paged_attend_scratch_bytes(int R, int n_q_heads, int n_kv_heads, int head_dim) {
+    if (R < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads != 0 || head_dim < 1 || head_dim > kMaxHeadDim) return 0;
+    return paged_attend_scratch_bytes(R, n_q_heads, n_kv_heads, head_dim);
+}
+
+extern "C" psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows, const int32_t* positions,
+                                        const uint8_t* skip, const psmc_rope* rope, const psmc_heads* k, const psmc_heads* v,
+                                        int n_q_heads, const psmc_heads* q, const psmc_heads* q_out, int32_t* status_word,
+                                        void* stream) {
+    TraceRange trace("psmc_paged_write");
+    PagedView c;
+    const psmc_status st = view_of(kv, &c);
+    if (st != PSMC_OK) return st;
+    return paged_write(c, n, rows, positions, skip, rope, k, v, n_q_heads, q, q_out, status_word, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" psmc_status psmc_paged_attend(const psmc_paged_kv* kv, const int32_t* lens, int extra, const uint8_t* skip,
+                                         int n_q_heads, const psmc_heads* q, const psmc_heads* out, float scale, float* lse,
+                                         void* scratch, size_t scratch_bytes, int32_t* status_word, void* stream) {
+    TraceRange trace("psmc_paged_attend");
+    PagedView c;
+    const psmc_status st = view_of(kv, &c);
+    if (st != PSMC_OK) return st;
+    return paged_attend(c, lens, extra, skip, n_q_heads, q, out, scale, lse, scratch, scratch_bytes, status_word,
+                        static_cast<cudaStream_t>(stream));
+}
+
+extern "C" psmc_status psmc_paged_read(const psmc_paged_kv* kv, const int32_t* lens, const uint8_t* skip, void* k_out,
+                                       void* v_out, int max_len, int64_t stride_row, int64_t stride_head, int32_t* status_word,
+                                       void* stream) {
+    TraceRange trace("psmc_paged_read");
+    PagedView c;
+    const psmc_status st = view_of(kv, &c);
+    if (st != PSMC_OK) return st;
+    return paged_read(c, lens, skip, k_out, v_out, max_len, stride_row, stride_head, status_word, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" psmc_status psmc_kv_paged_write(psmc_ctx* c, const psmc_kv_pools* pools, int layer, int n, const int32_t* rows,
+                                           const int32_t* positions, const psmc_rope* rope, const psmc_heads* k,
+                                           const psmc_heads* v, int n_q_heads, const psmc_heads* q, const psmc_heads* q_out,
+                                           void* stream) {
+    TraceRange trace("psmc_kv_paged_write");
+    psmc_paged_kv kv;
+    PagedView view;
+    psmc_status st = layer_of(c, pools, layer, &kv);
+    if (st == PSMC_OK) st = view_of(&kv, &view);
+    if (st != PSMC_OK) return st;
+    if ((rows == nullptr) != (positions == nullptr) || (!rows && n != c->R)) return PSMC_E_INVAL;
+    return paged_write(view, n, rows, rows ? positions : c->len, rows ? nullptr : done_now(c), rope, k, v, n_q_heads, q, q_out,
+                       c->status, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" psmc_status psmc_kv_paged_attend(psmc_ctx* c, const psmc_kv_pools* pools, int layer, int n_q_heads, const psmc_heads* q,
+                                            const psmc_heads* out, float scale, float* lse, void* scratch, size_t scratch_bytes,
+                                            void* stream) {
+    TraceRange trace("psmc_kv_paged_attend");
+    psmc_paged_kv kv;
+    PagedView view;
+    psmc_status st = layer_of(c, pools, layer, &kv);
+    if (st == PSMC_OK) st = view_of(&kv, &view);
+    if (st != PSMC_OK) return st;
+    return paged_attend(view, c->len, 1, done_now(c), n_q_heads, q, out, scale, lse, scratch, scratch_bytes, c->status,
+                        static_cast<cudaStream_t>(stream));
+}
+
+extern "C" psmc_status psmc_kv_paged_read(psmc_ctx* c, const psmc_kv_pools* pools, int layer, void* k_out, void* v_out, int max_len,
+                                          int64_t stride_row, int64_t stride_head, void* stream) {
+    TraceRange trace("psmc_kv_paged_read");
+    psmc_paged_kv kv;
+    PagedView view;
+    psmc_status st = layer_of(c, pools, layer, &kv);
+    if (st == PSMC_OK) st = view_of(&kv, &view);
+    if (st != PSMC_OK) return st;
+    return paged_read(view, c->len, nullptr, k_out, v_out, max_len, stride_row, stride_head, c->status,
+                      static_cast<cudaStream_t>(stream));
+}
+
 extern "C" psmc_status psmc_kv_paged_create(psmc_ctx* c, int n_blocks, int block_len, int max_blocks_per_row,
                                             int share_prompt) {
     if (!c || n_blocks < 1 || block_len < 1 || max_blocks_per_row < 1) return PSMC_E_INVAL;
@@ -649,10 +856,11 @@ extern "C" psmc_status psmc_reindex_kv_paged(psmc_ctx* c, const psmc_kv_pools* p
     if (!c->paged.table) return PSMC_E_STATE;
     if (pools->n_layers < 1 || pools->n_layers > kMaxKvPtrs / 2 || pools->n_kv_heads < 1 || pools->head_dim < 1)
         return PSMC_E_INVAL;
-    if (pools->dt != PSMC_F32 && pools->dt != PSMC_BF16) return PSMC_E_INVAL;
+    if (pools->dt != PSMC_F32 && pools->dt != PSMC_BF16 && pools->dt != PSMC_F8) return PSMC_E_INVAL;
     PagedPools pp;
     pp.n_layers = pools->n_layers; pp.H = pools->n_kv_heads;
-    pp.pos_bytes = pools->head_dim * (pools->dt == PSMC_F32 ? 4 : 2);
+    pp.pos_bytes = pools->head_dim * pool_elem_bytes(pools->dt);
+    pp.scale_bytes = pools->dt == PSMC_F8 ? (int)paged_scale_bytes(pools->n_kv_heads, c->paged.block_len) : 0;
     uint64_t bits = (uint64_t)pp.pos_bytes;
     for (int l = 0; l < pools->n_layers; ++l) {
         if (!pools->k[l] || !pools->v[l]) return PSMC_E_INVAL;

@@ -179,6 +179,7 @@ struct PagedPools {
     char* v[kMaxKvPtrs / 2];
     int n_layers, H;
     int pos_bytes;       // head_dim * sizeof(elem)
+    int scale_bytes;     // 8-bit pools: bytes behind a block's codes (scales and padding, a multiple of 16); else 0
 };
 size_t paged_free_list_words(int n_blocks, int R);  // words to allocate for PagedState::free_list
 cudaError_t launch_paged_init(const PagedState& ps, const int32_t* prompt_len_dev, int G, int share_prompt,
@@ -190,6 +191,62 @@ cudaError_t launch_paged_append(const PagedState& ps, const int32_t* len, const 
 cudaError_t launch_paged_reindex(const PagedState& ps, const PagedPools& pools, const MoveSource* sources,
                                  const int32_t* dst_rows, const int32_t* n_sources, const int32_t* n_moves,
                                  const int32_t* len, const uint8_t* done, int32_t* status, cudaStream_t stream);
+
+// ---------------------------------------------------------------- a language model's operators on the paged cache
+constexpr int kMaxHeadDim = 256;
+struct PagedView {       // one layer
+    char *k, *v;
+    const int32_t* table;
+    int64_t table_ld;
+    int R, n_blocks, block_len, max_blocks, H, D, dt;
+    int64_t blk_bytes;   // one block of one pool
+    int64_t scale_at;    // 8-bit pools: where a block's scale bytes begin
+};
+// scale bytes of a block, padded
+inline int64_t paged_scale_bytes(int H, int block_len) { return ((int64_t)H * block_len + 15) / 16 * 16; }
+
+struct HeadsView {       // [n, heads, D], unit stride along D
+    void* data;
+    int64_t stride_row, stride_head;  // elements
+};
+struct PagedWrite {
+    int n, Hq;
+    const int32_t* rows;       // NULL: token i belongs to row i
+    const int32_t* positions;
+    const uint8_t* skip;       // per row, may be NULL
+    const double* freqs;       // [rot / 2]
+    int rot, pairs;
+    float mscale;
+    int lanes_per_head;        // set by the launch
+    HeadsView k_in, v_in, q_in, q_out;
+    bool q;                    // q_in / q_out are given
+    int32_t* status;
+};
+cudaError_t launch_paged_write(const PagedView& c, const PagedWrite& w, cudaStream_t stream);
+
+struct PagedAttend {
+    const int32_t* lens;
+    int extra;                 // a row has lens[r] + extra positions
+    const uint8_t* skip;
+    int Hq;
+    HeadsView q, out;
+    float scale;
+    float* lse;                // [R, Hq], may be NULL
+    void* scratch;
+    int32_t* status;
+};
+size_t paged_attend_scratch_bytes(int R, int Hq, int H, int D);
+cudaError_t launch_paged_attend(const PagedView& c, const PagedAttend& a, cudaStream_t stream);
+
+struct PagedRead {
+    const int32_t* lens;
+    const uint8_t* skip;
+    void *k, *v;               // dense [R, H, max_len, D], either may be NULL
+    int64_t stride_row, stride_head;  // elements
+    int max_len;
+    int32_t* status;
+};
+cudaError_t launch_paged_read(const PagedView& c, const PagedRead& a, cudaStream_t stream);
 
 // ---------------------------------------------------------------- final draw and back-trace
 struct SelectArgs {

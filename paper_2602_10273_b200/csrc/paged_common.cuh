@@ -1,0 +1,73 @@
+// The paged cache as the operators of a language model see it: where a position's keys and values lie, and the
+// 8-bit form of a cache.
+//
+// Blocks of fp32 or bf16 pools are [H, block_len, D].  A block of an 8-bit pool holds the codes [H, block_len, D] (one
+// byte each: 4 exponent bits, 3 mantissa bits), then one scale byte per (head, position) [H, block_len], then padding
+// to 16 bytes.  The value of a code is code * 2^(byte - 127): a power of two loses nothing against any other scale,
+// because the codes are floating-point numbers themselves, and it keeps scaling and unscaling free of rounding.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace psmc {
+
+constexpr float kCodeMax = 448.f;   // largest finite code
+constexpr int kScaleLimit = 60;     // scale exponents lie in [-60, 60] (what this keeps in range: attention's sums)
+
+// elements of the tensors that go in and come out beside a pool of type DT
+template <int DT>
+struct PoolIo {
+    using type = __nv_bfloat16;
+};
+template <>
+struct PoolIo<PSMC_F32> {
+    using type = float;
+};
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// VEC consecutive elements of type T as one aligned access
+template <typename T, int VEC>
+struct alignas(sizeof(T) * VEC) Chunk {
+    T x[VEC];
+};
+
+// Smallest e with amax <= 448 * 2^e, within the limits; amax finite and >= 0.  448 = 1.75 * 2^8, so e is amax's own
+// exponent less 8, one more when its mantissa exceeds 1.75 (zero and subnormals end at the lower limit).
+__device__ __forceinline__ int scale_exponent(float amax) {
+    const uint32_t bits = __float_as_uint(amax);
+    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return min(max(e, -kScaleLimit), kScaleLimit);
+}
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // |e| <= 126
+
+__device__ __forceinline__ float code_value(uint8_t code) {
+    const __half_raw h = __nv_cvt_fp8_to_halfraw(code, __NV_E4M3);
+    return __half2float(__half(h));
+}
+// nearest code, ties to even, saturating; a non-finite component becomes the NaN code
+__device__ __forceinline__ uint8_t code_of(float y) {
+    return isfinite(y) ? (uint8_t)__nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3) : (uint8_t)0x7f;
+}
+
+// The block of position p of row r, or -1: outside the table, or an entry that names no block.
+__device__ __forceinline__ int block_of(const PagedView& c, int r, int j) {
+    if (j < 0 || j >= c.max_blocks) return -1;
+    const int blk = __ldg(c.table + (int64_t)r * c.table_ld + j);
+    return blk >= 0 && blk < c.n_blocks ? blk : -1;
+}
+
+}  // namespace psmc

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(256) paged_copy_kernel(const PagedState ps, co
     if (n <= 0) return;
     const CopyOrder* orders = orders_of(ps);
     const int n_pools = 2 * pools.n_layers;
-    const int64_t head_bytes = (int64_t)ps.block_len * pools.pos_bytes, blk_bytes = head_bytes * pools.H;
+    const int64_t head_bytes = (int64_t)ps.block_len * pools.pos_bytes, blk_bytes = head_bytes * pools.H + pools.scale_bytes;
     const int64_t total = (int64_t)n * n_pools;
     for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
         const int m = (int)(w / n_pools), q = (int)(w - (int64_t)m * n_pools);
@@ -212,6 +212,9 @@ __global__ void __launch_bounds__(256) paged_copy_kernel(const PagedState ps, co
             for (int u = 0; u < kBatch; ++u)
                 if (at[u] >= 0) dst[at[u]] = v[u];
         }
+        // 8-bit pools: all scale bytes of the block (those of positions that are not live yet mean nothing)
+        for (int e = threadIdx.x; e < pools.scale_bytes / 16; e += blockDim.x)
+            dst[pools.H * (int64_t)stride + e] = src[pools.H * (int64_t)stride + e];
     }
 }
 

@@ -1,0 +1,84 @@
+// The paged cache, gathered into dense tensors [R, H, max_len, D] (8-bit codes become the bf16 values they stand for,
+// exactly: a code has 4 significant bits).  Bound by bytes: every live position is read and written once.
+// A CTA takes one block of one row, keys or values: H x live positions x D, 16 bytes of output per lane and access.
+#include "paged_common.cuh"
+
+namespace psmc {
+namespace {
+
+constexpr int kReadThreads = 256;
+
+template <int DT, int VEC>
+__global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const PagedView c, const PagedRead a) {
+    using T = typename PoolIo<DT>::type;
+    chain_begin();
+    const int which = a.k && a.v ? (int)(blockIdx.y & 1) : (a.k ? 0 : 1);
+    const int r = a.k && a.v ? (int)(blockIdx.y >> 1) : (int)blockIdx.y, j = blockIdx.x;
+    if (a.skip && a.skip[r]) return;
+    int n = __ldg(a.lens + r);
+    if (n > a.max_len || n > c.max_blocks * (int64_t)c.block_len) {
+        if (j == 0 && threadIdx.x == 0) raise_status(a.status, PSMC_E_STATE);
+        n = (int)min((int64_t)a.max_len, c.max_blocks * (int64_t)c.block_len);
+    }
+    const int64_t p0 = (int64_t)j * c.block_len;
+    if (p0 >= n) return;
+    const int live = (int)min((int64_t)c.block_len, n - p0);
+    const int blk = block_of(c, r, j);
+    if (blk < 0) {
+        if (threadIdx.x == 0) raise_status(a.status, PSMC_E_STATE);
+        return;
+    }
+    const char* pool = (which ? c.v : c.k) + (int64_t)blk * c.blk_bytes;
+    T* dst = static_cast<T*>(which ? a.v : a.k) + (int64_t)r * a.stride_row + p0 * c.D;
+    const int per_pos = c.D / VEC, per_head = live * per_pos;
+    for (int e = threadIdx.x; e < per_head * c.H; e += kReadThreads) {
+        const int h = e / per_head, x = e - h * per_head, o = x / per_pos, d = (x - o * per_pos) * VEC;
+        const int64_t from = ((int64_t)h * c.block_len + o) * c.D + d;
+        Chunk<T, VEC> out;
+        if (DT == PSMC_F8) {
+            const Chunk<uint8_t, VEC> in = *reinterpret_cast<const Chunk<uint8_t, VEC>*>(pool + from);
+            const float scale = pow2i((int)reinterpret_cast<const uint8_t*>(pool)[c.scale_at + (int64_t)h * c.block_len + o] - 127);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) out.x[i] = from_float<T>(code_value(in.x[i]) * scale);
+        } else {
+            out = *reinterpret_cast<const Chunk<T, VEC>*>(pool + from * sizeof(T));
+        }
+        *reinterpret_cast<Chunk<T, VEC>*>(dst + (int64_t)h * a.stride_head + (int64_t)o * c.D + d) = out;
+    }
+}
+
+template <int DT>
+cudaError_t launch(const PagedView& c, const PagedRead& a, cudaStream_t stream) {
+    using T = typename PoolIo<DT>::type;
+    constexpr int kFullVec = 16 / sizeof(T);
+    uint64_t bits = (uint64_t)(a.stride_row * sizeof(T)) | (uint64_t)(a.stride_head * sizeof(T)) | (uint64_t)(uintptr_t)a.k |
+                    (uint64_t)(uintptr_t)a.v;
+    // 16 bytes per access where every destination row starts on such a boundary, else one element
+    auto fn = bits % 16 == 0 && c.D % kFullVec == 0 ? paged_read_kernel<DT, kFullVec> : paged_read_kernel<DT, 1>;
+    const int rows_per_launch = 1 << 14;  // grid.y limit
+    const int64_t max_pos = c.max_blocks * (int64_t)c.block_len < a.max_len ? c.max_blocks * (int64_t)c.block_len : a.max_len;
+    const unsigned blocks = (unsigned)((max_pos + c.block_len - 1) / c.block_len);
+    for (int r0 = 0; r0 < c.R; r0 += rows_per_launch) {
+        PagedView cc = c;
+        PagedRead aa = a;
+        cc.R = c.R - r0 < rows_per_launch ? c.R - r0 : rows_per_launch;
+        cc.table = c.table + (int64_t)r0 * c.table_ld;
+        aa.lens = a.lens + r0;
+        if (a.skip) aa.skip = a.skip + r0;
+        if (a.k) aa.k = static_cast<T*>(a.k) + (int64_t)r0 * a.stride_row;
+        if (a.v) aa.v = static_cast<T*>(a.v) + (int64_t)r0 * a.stride_row;
+        const cudaError_t e = launch_chained(fn, dim3(blocks, (unsigned)cc.R * (a.k && a.v ? 2 : 1)), dim3(kReadThreads), 0, stream, cc, aa);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_paged_read(const PagedView& c, const PagedRead& a, cudaStream_t stream) {
+    if (c.R <= 0 || a.max_len <= 0) return cudaSuccess;
+    if (c.dt == PSMC_F32) return launch<PSMC_F32>(c, a, stream);
+    return c.dt == PSMC_BF16 ? launch<PSMC_BF16>(c, a, stream) : launch<PSMC_F8>(c, a, stream);
+}
+
+}  // namespace psmc

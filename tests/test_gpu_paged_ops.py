@@ -1,0 +1,630 @@
+"""Rotary write, attention and read-back on the paged cache, against the 64-bit definitions of tests/paged_reference.py."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as PR
+from paper_2602_10273_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+IO = {"f32": torch.float32, "bf16": torch.bfloat16, "f8": torch.bfloat16}
+# how attention rounds its weights before they meet the values: not at all for fp32 caches; to a sum of two bf16 numbers
+# for bf16 caches (the first within 2^-8 of the weight, the second within 2^-8 of the rest); to fp16 for 8-bit ones, half
+# a step 2^-11 and, for weights under 2^-14 of the largest, 2^-25 of it each (at most 4096 such positions in these tests)
+WEIGHT_STEP = {"f32": 0.0, "bf16": 2.0 ** -16, "f8": 2.0 ** -11 + 4096 * 2.0 ** -25}
+
+
+class Cache:
+    """Random pools, table and lengths.  share: rows r with equal r // share use the same blocks where both are full."""
+
+    def __init__(self, dt, lens, H, D, page, seed=0, share=1, spare_cols=0, nan_elsewhere=True, magnitude=1.0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.dt, self.H, self.D, self.page, self.R = dt, H, D, page, len(lens)
+        self.lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        mb = max(1, -(-max(lens) // page)) + spare_cols
+        rng = np.random.default_rng(seed)
+        table, n = np.full((self.R, mb), -1, np.int64), 0
+        for r, ln in enumerate(lens):
+            lead = r - r % share
+            for j in range(-(-ln // page)):
+                both_full = min(ln, lens[lead]) >= (j + 1) * page
+                # a shared leading part, then private blocks: the last third of a row is its own
+                if r != lead and both_full and j < (2 * ln) // (3 * page):
+                    table[r, j] = table[lead, j]
+                else:
+                    table[r, j], n = n, n + 1
+        self.n_blocks = n + 2
+        place = rng.permutation(self.n_blocks)
+        self.table = torch.from_numpy(np.where(table >= 0, place[table], -1).astype(np.int32)).cuda()
+        shape = (self.n_blocks, H, page, D)
+        self.pools = []
+        for _ in range(2):
+            x = torch.randn(shape, device="cuda", generator=g) * magnitude
+            if dt == "f8":
+                x = x * torch.exp2(torch.randint(-6, 7, shape[:3] + (1,), device="cuda", generator=g).float())
+                e, q = PR.quantise(x.double())
+                y = torch.ldexp(q, -e[..., None])          # codes as values
+                raw = torch.zeros((self.n_blocks, B.paged_block_bytes(H, page, D, B.F8)), dtype=torch.uint8, device="cuda")
+                raw[:, : H * page * D] = y.float().to(torch.float8_e4m3fn).view(torch.uint8).view(self.n_blocks, -1)
+                raw[:, H * page * D: H * page * D + H * page] = (e + 127).to(torch.uint8).view(self.n_blocks, -1)
+                x = raw
+            else:
+                x = x.to(IO[dt])
+            self.pools.append(x)
+        if nan_elsewhere:
+            self.poison()
+        self.handle = B.PagedKv(self.pools[0], self.pools[1], self.table, H, D, page)
+
+    def poison(self):
+        """Whatever no row's live positions reach holds NaN (8-bit: the NaN code, and a scale byte of 255)."""
+        H, D, page = self.H, self.D, self.page
+        dead = torch.ones((self.n_blocks, page), dtype=torch.bool, device="cuda")
+        for r, ln in enumerate(self.lens.tolist()):
+            pos = torch.arange(ln, device="cuda")
+            dead[self.table[r, pos // page].long(), pos % page] = False
+        for p in self.pools:
+            if self.dt == "f8":
+                n = self.n_blocks
+                codes = p[:, : H * page * D].view(n, H, page, D)
+                codes.copy_(torch.where(dead[:, None, :, None], 127, codes))
+                sc = p[:, H * page * D: H * page * D + H * page].view(n, H, page)
+                sc.copy_(torch.where(dead[:, None, :], 255, sc))
+            else:
+                p.masked_fill_(dead[:, None, :, None], math.nan)
+
+    def values(self):
+        return [PR.pool_values(p, self.H, self.page, self.D) for p in self.pools]
+
+
+def check_attend(c, q, out, lse, scale, extra=0, rows=None):
+    kv, vv = c.values()
+    for r in (range(c.R) if rows is None else rows):
+        n = int(c.lens[r]) + extra
+        want, want_lse, absv, reach = PR.attend(q[r], PR.row_values(kv, c.table, r, n), PR.row_values(vv, c.table, r, n), scale)
+        bound = PR.attend_bound(want, absv, reach, n, c.D, q.dtype, WEIGHT_STEP[c.dt])
+        off = (out[r].double() - want).abs()
+        assert (off <= bound).all(), "row %d (%d positions): %.3g over a bound of %.3g" % (
+            r, n, float(off.max()), float(bound.flatten()[off.argmax()]))
+        if lse is not None:
+            if n == 0:
+                assert (lse[r] == -math.inf).all()
+            else:
+                u = 2.0 ** -24
+                tol = (c.D + 10) * u * reach + (n + 80) * u + 4 * u * want_lse.abs()
+                assert ((lse[r].double() - want_lse).abs() <= tol).all()
+
+
+SHAPES = [  # dt, H, queries per key-value head, D, page, lens, share
+    ("f32", 2, 2, 64, 16, [0, 1, 15, 16, 17, 121], 1),
+    ("f32", 1, 7, 20, 5, [3, 0, 300, 64], 1),
+    ("f32", 3, 1, 4, 16, [33, 34], 2),
+    ("f32", 2, 9, 256, 16, [50, 50, 50], 3),
+    ("f32", 2, 4, 128, 16, [400, 400, 401, 399], 4),
+    ("bf16", 2, 4, 128, 16, [0, 1, 2, 15, 16, 17, 31, 32, 33, 500], 1),
+    ("bf16", 4, 7, 128, 16, [700] * 16, 16),
+    ("bf16", 32, 1, 128, 16, [257, 255, 300, 120, 300, 300, 300, 300], 8),
+    ("bf16", 1, 8, 64, 7, [100, 100, 41], 3),
+    ("bf16", 2, 33, 64, 16, [90, 1, 160], 1),
+    ("bf16", 2, 16, 8, 16, [90, 7], 2),
+    ("bf16", 1, 3, 80, 1, [65, 129, 2], 3),
+    ("bf16", 1, 2, 256, 128, [1000, 127, 128, 129], 1),
+    ("bf16", 2, 5, 248, 3, [77, 200, 200], 2),
+    ("bf16", 8, 4, 128, 16, [64 + 13 * g for g in range(9) for _ in range(8)], 8),
+    ("bf16", 1, 4, 96, 64, [20000], 1),
+    ("bf16", 2, 4, 128, 16, [2000] * 70, 35),
+    ("f8", 2, 4, 128, 16, [0, 1, 2, 15, 16, 17, 31, 32, 33, 500], 1),
+    ("f8", 4, 7, 128, 16, [1100] * 32, 32),
+    ("f8", 1, 8, 64, 7, [100, 100, 41], 3),
+    ("f8", 3, 4, 16, 5, [90, 1, 160, 160], 4),
+    ("f8", 2, 1, 256, 32, [130, 999], 1),
+    ("f8", 2, 20, 80, 8, [333, 333, 332], 3),
+    ("f8", 1, 4, 112, 16, [4000], 1),
+]
+
+
+@pytest.mark.parametrize("dt,H,ratio,D,page,lens,share", SHAPES, ids=lambda v: str(v)[:24].replace(" ", ""))
+def test_attend(dt, H, ratio, D, page, lens, share):
+    c = Cache(dt, lens, H, D, page, seed=5, share=share, spare_cols=3)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    q = (1.5 * torch.randn((c.R, H * ratio, D), device="cuda", generator=g)).to(IO[dt])
+    lse = torch.full((c.R, H * ratio), 7.0, device="cuda")
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    scale = D ** -0.5
+    out = B.paged_attend(c.handle, q, c.lens, scale, lse=lse, status_word=word)
+    check_attend(c, q, out, lse, scale)
+    assert int(word) == B.OK
+    again = B.paged_attend(c.handle, q, c.lens, scale)
+    assert torch.equal(out, again)                      # the same bits every time: no sum depends on an order of arrival
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f8"])
+def test_attend_strides_skip_extra_and_scale(dt):
+    """Queries that are part of a projection's output, an out with gaps, finished rows, the position just written."""
+    H, ratio, D, page = 2, 4, 64, 16
+    c = Cache(dt, [40, 17, 300, 16, 16], H, D, page, seed=3)
+    c.lens -= 1                                         # extra = 1 restores it
+    qkv = torch.randn((5, (ratio + 2) * H, D), device="cuda").to(IO[dt])
+    q = qkv[:, : ratio * H]
+    big = torch.full((5, ratio * H, 3 * D), 3.0, dtype=IO[dt], device="cuda")
+    out, lse = big[:, :, D: 2 * D], torch.full((5, ratio * H), 7.0, device="cuda")
+    skip = torch.tensor([0, 1, 0, 0, 1], dtype=torch.uint8, device="cuda")
+    B.paged_attend(c.handle, q, c.lens, -0.3, out=out, lse=lse, skip=skip, extra=1)
+    check_attend(c, q, out, lse, -0.3, extra=1, rows=[0, 2, 3])
+    assert (out[[1, 4]] == 3.0).all() and (lse[[1, 4]] == 7.0).all()
+    assert (big[:, :, :D] == 3.0).all() and (big[:, :, 2 * D:] == 3.0).all()
+    # scale 0: the mean of the values, whatever the keys
+    out = B.paged_attend(c.handle, q, c.lens, 0.0, skip=skip, extra=1)
+    check_attend(c, q, out, None, 0.0, extra=1, rows=[0, 2, 3])
+    assert (out[1] == 0).all()                          # allocated here: zeros where rows were left out
+    # a query off the 4-byte boundary (bf16), and a table whose rows are wider than what is used
+    odd = torch.empty(5 * ratio * H * D + 1, dtype=IO[dt], device="cuda")[1:].view(5, ratio * H, D)
+    odd.copy_(q)
+    assert torch.equal(B.paged_attend(c.handle, odd, c.lens, 0.3, extra=1), B.paged_attend(c.handle, q.contiguous(), c.lens, 0.3, extra=1))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f8"])
+def test_attend_large_scores_and_far_maxima(dt):
+    """Scores of hundreds, the maximum at the first, a middle and the last position, other rows' scores very negative."""
+    H, ratio, D, page = 1, 4, 64, 16
+    c = Cache(dt, [200, 200, 200, 200], H, D, page, seed=11, magnitude=4.0)
+    q = (12 * torch.randn((4, ratio, D), device="cuda")).to(IO[dt])
+    out = B.paged_attend(c.handle, q, c.lens, 1.0)
+    check_attend(c, q, out, None, 1.0)
+
+
+def test_attend_does_not_mix_rows_or_heads_that_hold_nan():
+    """A NaN in a live key or value reaches the heads that read it, and nothing else."""
+    H, ratio, D, page = 2, 4, 64, 16
+    for dt in ("f32", "bf16", "f8"):
+        c = Cache(dt, [100, 100, 100, 100], H, D, page, seed=2, share=4)
+        q = torch.randn((4, H * ratio, D), device="cuda").to(IO[dt])
+        clean = B.paged_attend(c.handle, q, c.lens, 0.1)
+        blk = int(c.table[2, 6])                        # the last block: row 2's own
+        if dt == "f8":
+            c.pools[0][blk, : H * page * D].view(H, page, D)[1, 2, 5] = 127
+        else:
+            c.pools[0][blk, 1, 2, 5] = math.nan
+        out = B.paged_attend(c.handle, q, c.lens, 0.1)
+        assert out[2, ratio:].isnan().all()
+        keep = torch.ones(4, H * ratio, dtype=torch.bool, device="cuda")
+        keep[2, ratio:] = False
+        assert torch.equal(out[keep], clean[keep])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f8"])
+def test_attend_reports_bad_tables_and_lengths(dt):
+    H, D, page = 2, 64, 16
+    c = Cache(dt, [64, 64, 64], H, D, page, seed=1)
+    q = torch.randn((3, 4, D), device="cuda").to(IO[dt])
+    good = B.paged_attend(c.handle, q, c.lens, 0.1)
+    for bad in (-1, -(1 << 31), c.n_blocks, (1 << 31) - 1):
+        word, keep = torch.zeros(1, dtype=torch.int32, device="cuda"), int(c.table[1, 2])
+        c.table[1, 2] = bad
+        out = B.paged_attend(c.handle, q, c.lens, 0.1, status_word=word)
+        assert int(word) == B.E_STATE
+        assert torch.equal(out[[0, 2]], good[[0, 2]])   # the others are as they should be
+        c.table[1, 2] = keep
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    long = torch.tensor([64, 65, 64], dtype=torch.int32, device="cuda")
+    out = B.paged_attend(c.handle, q, long, 0.1, status_word=word)
+    assert int(word) == B.E_STATE and torch.equal(out, good)
+    word.zero_()
+    neg = torch.tensor([64, -5, 64], dtype=torch.int32, device="cuda")
+    out = B.paged_attend(c.handle, q, neg, 0.1, status_word=word)
+    assert int(word) == B.OK and (out[1] == 0).all() and torch.equal(out[[0, 2]], good[[0, 2]])
+
+
+def test_attend_far_beyond_32_bit_offsets():
+    """Blocks whose bytes and elements lie beyond 2^32."""
+    H, D, page, n_blocks = 8, 128, 16, 135000            # 4.4 GB a pool, 2.2 G elements
+    k = torch.zeros((n_blocks, H, page, D), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    c = Cache("bf16", [70, 33], H, D, page, seed=4)
+    far = torch.arange(n_blocks - c.n_blocks, n_blocks, device="cuda")
+    k[far], v[far] = c.pools[0], c.pools[1]
+    table = torch.where(c.table >= 0, c.table + (n_blocks - c.n_blocks), c.table).to(torch.int32)
+    h = B.PagedKv(k, v, table, H, D, page)
+    q = torch.randn((2, 32, D), device="cuda").to(torch.bfloat16)
+    assert torch.equal(B.paged_attend(h, q, c.lens, 0.1), B.paged_attend(c.handle, q, c.lens, 0.1))
+    dense = [torch.zeros((2, H, 80, D), dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    B.paged_read(h, c.lens, dense[0], dense[1])
+    B.paged_read(c.handle, c.lens, dense[2], dense[3])
+    assert torch.equal(dense[0], dense[2]) and torch.equal(dense[1], dense[3]) and dense[0].abs().sum() > 0
+    rows, pos = torch.tensor([0, 1], dtype=torch.int32, device="cuda"), torch.tensor([69, 32], dtype=torch.int32, device="cuda")
+    x = torch.randn((2, H, D), device="cuda").to(torch.bfloat16)
+    B.paged_write(h, x, x, rows, pos)
+    assert torch.equal(k[table[0, 4].long(), :, 5], x[0]) and torch.equal(v[table[1, 2].long(), :, 0], x[1])
+
+
+# ---------------------------------------------------------------- write and read
+WRITES = [  # dt, H, Hq, D, page, rot, layout, scaling
+    ("f32", 2, 4, 64, 16, 64, "half", "none"),
+    ("f32", 1, 3, 20, 5, 6, "pairs", "linear"),
+    ("f32", 2, 2, 256, 16, 256, "half", "yarn"),
+    ("f32", 1, 1, 4, 3, 2, "half", "none"),
+    ("bf16", 8, 32, 128, 16, 128, "half", "bands"),
+    ("bf16", 4, 28, 128, 16, 64, "pairs", "yarn"),
+    ("bf16", 2, 2, 80, 1, 60, "half", "base"),
+    ("bf16", 1, 5, 256, 128, 250, "pairs", "none"),
+    ("bf16", 3, 3, 8, 16, 0, "half", "none"),
+    ("f8", 8, 32, 128, 16, 128, "half", "bands"),
+    ("f8", 2, 4, 64, 7, 62, "half", "none"),
+    ("f8", 1, 1, 256, 16, 256, "pairs", "linear"),
+    ("f8", 3, 3, 16, 5, 4, "half", "none"),
+]
+
+
+def _rope(rot, layout, scaling):
+    if rot == 0:
+        return None, torch.zeros(0, dtype=torch.float64, device="cuda"), 1.0
+    f, m = B.rope_frequencies(rot, 10000.0, scaling, 1.0 if scaling == "none" else 8.0, 1.0, 32.0, 4096)
+    f = torch.from_numpy(f).cuda()
+    return B.Rope(f, layout, m), f, m
+
+
+@pytest.mark.parametrize("dt,H,Hq,D,page,rot,layout,scaling", WRITES, ids=lambda v: str(v))
+@pytest.mark.parametrize("offset", [0, 1])
+def test_write_then_read(dt, H, Hq, D, page, rot, layout, scaling, offset):
+    """Tokens in any order at positions near and far; offset 1 puts inputs off every vector boundary."""
+    R, n_far = 3, 100000
+    mb = -(-n_far // page) + 1
+    lens = [37, 1, 20]
+    table = torch.full((R, mb), -1, dtype=torch.int32, device="cuda")
+    blocks = list(np.random.default_rng(1).permutation(200))
+    todo = [(r, p) for r in range(R) for p in range(lens[r])] + [(1, n_far), (2, n_far - 1)]
+    for r, p in todo:
+        if table[r, p // page] < 0:
+            table[r, p // page] = int(blocks.pop())
+    todo = [todo[i] for i in np.random.default_rng(2).permutation(len(todo))]
+    n = len(todo)
+    rows = torch.tensor([r for r, _ in todo], dtype=torch.int32, device="cuda")
+    pos = torch.tensor([p for _, p in todo], dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(6)
+
+    def tokens(heads):
+        t = torch.empty(n * heads * D + offset, dtype=IO[dt], device="cuda")[offset:].view(n, heads, D)
+        return t.copy_(torch.randn((n, heads, D), device="cuda", generator=g) * 3)
+
+    k, v, q = tokens(H), tokens(H), tokens(Hq)
+    k[3] = 0                                             # an all-zero head
+    v[4, 0, : D // 2] *= 2.0 ** 40
+    nb = B.paged_block_bytes(H, page, D, B.F8)
+    shape, ty = ((200, nb), torch.uint8) if dt == "f8" else ((200, H, page, D), IO[dt])
+    kp, vp = [torch.full(shape, 77, dtype=ty, device="cuda") for _ in range(2)]
+    cache = B.PagedKv(kp, vp, table, H, D, page)
+    rope, freqs, m = _rope(rot, layout, scaling)
+    q0 = q.clone()
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q_out = B.paged_write(cache, k, v, rows, pos, q=q, rope=rope, status_word=word)
+    assert int(word) == B.OK and torch.equal(q, q0)
+    # Rotation: the cosine and sine of the kernel are within 3 u of the exact ones (u = 2^-24: the fraction of a turn is
+    # kept to first order beyond 32 bits, the functions are good to 2 ulp, mscale adds one rounding), each product and the
+    # sum round once more: 6 u (|a| + |b|) mscale; then the type's rounding.
+    u = 2.0 ** -24
+
+    def check_rotated(got, x):
+        want = PR.rotate(x, pos, freqs, layout, m)
+        size = x.double().abs().amax(-1, keepdim=True) * 2 * m
+        tol = 6 * u * size + PR.HALF_STEP[IO[dt]] * want.abs() + 1e-45
+        assert ((got.double() - want).abs() <= tol).all()
+        assert torch.equal(got[..., rot:], x[..., rot:])
+        return want
+
+    check_rotated(q_out, q0)
+    q_same = q.clone()
+    B.paged_write(cache, k, v, rows, pos, q=q_same, q_out=q_same, rope=rope)   # in place
+    assert torch.equal(q_same, q_out)
+    blk, off = table[rows.long(), pos.long() // page].long(), pos.long() % page
+    if dt != "f8":
+        check_rotated(kp[blk, :, off], k)
+        assert torch.equal(vp[blk, :, off], v)
+    else:
+        codes = [p[:, : H * page * D].view(200, H, page, D)[blk, :, off] for p in (kp, vp)]
+        exps = [p[:, H * page * D: H * page * D + H * page].view(200, H, page)[blk, :, off].long() - 127 for p in (kp, vp)]
+        e, val = PR.quantise(v.double())
+        assert torch.equal(exps[1], e)
+        assert torch.equal(torch.ldexp(PR.code_values(codes[1]), e[..., None]), val)       # no rounding before the code
+        kr = PR.rotate(k, pos, freqs, layout, m)
+        slack = 6 * u * k.double().abs().amax(-1, keepdim=True) * 2 * m
+        top = kr.abs().amax(-1, keepdim=True)
+        scale = torch.ldexp(torch.ones_like(kr), exps[0][..., None].expand_as(kr))
+        assert (top - slack <= 448 * scale[..., :1]).all()
+        assert ((top + slack > 224 * scale[..., :1]) | (exps[0][..., None] == -60)).all()   # the smallest that is enough
+        got = PR.code_values(codes[0]) * scale
+        half = torch.maximum(kr.abs() * 2.0 ** -4, scale * 2.0 ** -10)
+        assert ((got - kr).abs() <= half + slack * (1 + 2.0 ** -3)).all()
+    # nothing else was touched
+    live = torch.zeros((200, page), dtype=torch.bool, device="cuda")
+    live[blk, off] = True
+    for p in (kp, vp):
+        if dt != "f8":
+            assert (p.permute(0, 2, 1, 3)[~live] == 77).all()
+        else:
+            assert (p[:, : H * page * D].view(200, H, page, D).permute(0, 2, 1, 3)[~live] == 77).all()
+            assert (p[:, H * page * D: H * page * D + H * page].view(200, H, page).permute(0, 2, 1)[~live] == 77).all()
+            assert (p[:, H * page * D + H * page:] == 77).all()
+    # read back: what the pools hold, exactly; odd destinations take the other access path
+    lens_t = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ml = 41
+    dense = [torch.empty(R * H * (ml * D + 3) + offset, dtype=IO[dt], device="cuda")[offset:].fill_(5).view(R, H, ml * D + 3)[..., : ml * D].unflatten(2, (ml, D))
+             for _ in range(2)]
+    B.paged_read(cache, lens_t, dense[0], dense[1], status_word=word)
+    one = [torch.full((R, H, ml, D), 5.0, dtype=IO[dt], device="cuda") for _ in range(2)]
+    B.paged_read(cache, lens_t, k_out=one[0])
+    B.paged_read(cache, lens_t, v_out=one[1])
+    for pool, d, o in zip((kp, vp), dense, one):
+        vals = PR.pool_values(pool, H, page, D)
+        for r, ln in enumerate(lens):
+            assert torch.equal(d[r, :, :ln].double(), PR.row_values(vals, table, r, ln))
+            assert (d[r, :, ln:] == 5).all()
+        assert torch.equal(d, o)
+    assert int(word) == B.OK
+
+
+def test_write_padding_skip_and_bad_positions():
+    H, D, page, R = 2, 64, 16, 3
+    for dt in ("f32", "bf16", "f8"):
+        shape, ty = ((8, B.paged_block_bytes(H, page, D, B.F8)), torch.uint8) if dt == "f8" else ((8, H, page, D), IO[dt])
+        kp, vp = [torch.zeros(shape, dtype=ty, device="cuda") for _ in range(2)]
+        table = torch.tensor([[0, 1], [2, -1], [3, 99]], dtype=torch.int32, device="cuda")
+        cache = B.PagedKv(kp, vp, table, H, D, page)
+        #        pad  ok  skip  no block  bad entry  beyond  negative  bad row
+        rows = [-1, 0, 1, 1, 2, 0, 0, 3]
+        pos = [0, 17, 3, 16, 16, 32, -1, 0]
+        x = torch.randn((8, H, D), device="cuda").to(IO[dt])
+        q_out = torch.full_like(x, 9.0)
+        t = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+        skip = torch.tensor([0, 1, 0], dtype=torch.uint8, device="cuda")
+        for drop, want in (([3, 4, 5, 6, 7], B.OK), ([3, 5, 6, 7], B.E_STATE), ([3, 4, 6, 7], B.E_STATE), ([3, 4, 5, 7], B.E_STATE),
+                           ([3, 4, 5, 6], B.E_STATE)):
+            keep = [i for i in range(8) if i not in drop]
+            word = torch.zeros(1, dtype=torch.int32, device="cuda")
+            q_out.fill_(9.0)
+            got = B.paged_write(cache, x[keep], x[keep], t([rows[i] for i in keep]), t([pos[i] for i in keep]), q=x[keep],
+                                q_out=q_out[: len(keep)], skip=skip, status_word=word)
+            assert int(word) == want
+            assert torch.equal(got[keep.index(1)], x[1])
+            assert (got[[keep.index(i) for i in keep if i != 1]] == 9.0).all()
+        for p in (kp, vp):
+            assert (p[[0, 2, 3, 4, 5, 6, 7]] == 0).all() and (p[1] != 0).any()
+        # no rows: token i is row i's
+        B.paged_write(cache, x[:3], x[:3], None, t([1, 2, 3]), skip=skip)
+        assert (p[0] != 0).any() and (p[2] == 0).all() and (p[3] != 0).any()
+        # one token without any position in range must not stop a call of none
+        assert B.paged_write(cache, x[:0], x[:0], t([]), t([])) is None
+
+
+def test_write_non_finite_components():
+    """bf16 and fp32 caches keep them; 8-bit caches hold NaN in their place and scale by the finite ones."""
+    H, D, page = 1, 64, 16
+    v = torch.randn((1, H, D), device="cuda")
+    v[0, 0, 3], v[0, 0, 4], v[0, 0, 5] = math.inf, -math.inf, math.nan
+    table = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    pos = torch.tensor([7], dtype=torch.int32, device="cuda")
+    for dt in ("f32", "bf16"):
+        kp, vp = [torch.zeros((1, H, page, D), dtype=IO[dt], device="cuda") for _ in range(2)]
+        B.paged_write(B.PagedKv(kp, vp, table, H, D, page), v.to(IO[dt]), v.to(IO[dt]), None, pos)
+        assert torch.equal(vp[0, 0, 7].nan_to_num(1e3), v[0, 0].to(IO[dt]).nan_to_num(1e3))
+    kp, vp = [torch.zeros((1, B.paged_block_bytes(H, page, D, B.F8)), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    c = B.PagedKv(kp, vp, table, H, D, page)
+    big = v.clone()
+    big[0, 0, 10] = 1e30                                 # beyond the largest scale: saturates
+    for x in (v, big):
+        B.paged_write(c, x.bfloat16(), x.bfloat16(), None, pos)
+        got = PR.pool_values(vp, H, page, D)[0, 0, 7]
+        e, want = PR.quantise(x.bfloat16().double()[0, 0])
+        assert torch.equal(got.isnan(), want.isnan()) and int(got.isnan().sum()) == 3
+        assert torch.equal(got.nan_to_num(0), want.nan_to_num(0))
+    assert got[10] == 448.0 * 2.0 ** 60
+
+
+def test_read_skips_clips_and_reports():
+    c = Cache("bf16", [40, 17, 0, 30], 2, 64, 16, seed=8)
+    d = [torch.full((4, 2, 32, 64), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    skip = torch.tensor([0, 0, 0, 1], dtype=torch.uint8, device="cuda")
+    B.paged_read(c.handle, c.lens, d[0], d[1], skip=skip, status_word=word)   # row 0 is longer than the destination
+    assert int(word) == B.E_STATE
+    vals = c.values()
+    for x, y in zip(d, vals):
+        assert torch.equal(x[0].double(), PR.row_values(y, c.table, 0, 32))
+        assert torch.equal(x[1, :, :17].double(), PR.row_values(y, c.table, 1, 17))
+        assert (x[1, :, 17:] == 5).all() and (x[2:] == 5).all()
+    word.zero_()
+    c.table[1, 1] = c.n_blocks
+    lens = c.lens.clone()
+    lens[0] = 20
+    d[0].fill_(5.0)
+    B.paged_read(c.handle, lens, d[0], d[1], skip=skip, status_word=word)
+    assert int(word) == B.E_STATE
+    assert torch.equal(d[0][1, :, :16].double(), PR.row_values(vals[0], c.table, 1, 16)) and (d[0][1, :, 16:] == 5).all()
+
+
+def test_streams_and_graphs():
+    """On another stream than the current one; captured and replayed with new lengths, queries and table entries."""
+    H, ratio, D, page = 2, 4, 128, 16
+    c = Cache("bf16", [200, 90, 300, 16], H, D, page, seed=12, nan_elsewhere=False)
+    q = torch.randn((4, H * ratio, D), device="cuda").to(torch.bfloat16)
+    want = B.paged_attend(c.handle, q, c.lens, 0.1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = B.paged_attend(c.handle, q, c.lens, 0.1, stream=side)
+    raw = B.paged_attend(c.handle, q, c.lens, 0.1, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(raw, want)
+
+    out = [torch.empty_like(q) for _ in range(2)]
+    lens, qs = c.lens.clone(), q.clone()
+    pos = torch.tensor([199, 89, 299, 15], dtype=torch.int32, device="cuda")
+    kv = torch.randn((4, H, D), device="cuda").to(torch.bfloat16)
+    graphs = []
+    for o in out:                                        # two graphs, which must not share a workspace
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            B.paged_write(c.handle, kv, kv, None, pos)
+            B.paged_attend(c.handle, qs, lens, 0.1, out=o)
+        graphs.append(gr)
+    lens.copy_(torch.tensor([7, 0, 299, 33], dtype=torch.int32))
+    pos[3] = 15
+    qs.mul_(2)
+    kv.mul_(-1)
+    c.table[[0, 2], 0] = c.table[[2, 0], 0]
+    torch.cuda.synchronize()
+    s2 = torch.cuda.Stream()
+    for _ in range(20):                                  # side by side on two streams
+        with torch.cuda.stream(side):
+            graphs[0].replay()
+        with torch.cuda.stream(s2):
+            graphs[1].replay()
+    torch.cuda.synchronize()
+    lens[3] = 16
+    for gr in graphs:
+        gr.replay()
+    torch.cuda.synchronize()
+    c.lens = lens
+    check_attend(c, qs, out[0], None, 0.1)
+    assert torch.equal(out[0], out[1])
+    assert torch.equal(c.pools[0][c.table[0, 12].long(), :, 7], kv[0])
+
+
+def test_two_calls_at_once_on_one_cache():
+    c = Cache("f8", [4000] * 8, 4, 128, 16, seed=13, share=8)
+    q = [torch.randn((8, 28, 128), device="cuda").to(torch.bfloat16) for _ in range(2)]
+    want = [B.paged_attend(c.handle, x, c.lens, 0.1) for x in q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(B.paged_attend(c.handle, q[i], c.lens, 0.1))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in outs[i])
+
+
+# ---------------------------------------------------------------- together, in the loop of the particle system
+@pytest.mark.parametrize("dt,G,N,H,ratio,D,page,share", [("bf16", 3, 8, 2, 4, 64, 8, True), ("f8", 2, 16, 2, 2, 64, 16, True),
+                                                         ("f32", 2, 4, 1, 3, 32, 4, False)])
+def test_decode_loop_with_resampling(dt, G, N, H, ratio, D, page, share):
+    """Two layers of write and attend per token, psmc_step, copy-on-write reindex, 60 tokens: every layer's attention
+    against a dense mirror in 64 bits that is moved by the slot map, and the cache read back against the same mirror."""
+    T, V, L = 60, 64, 2
+    prompt = [5 + 7 * g for g in range(G)]
+    ps = B.init_batched(G, N, V, 4.0, 0.25, 0.9, 0, 7, 1, T_max=T, prompt_len=prompt)
+    R, ML = ps.R, max(prompt) + T + 1
+    MB = -(-ML // page)
+    n_blocks = R * MB
+    ps.kv_paged_create(n_blocks, page, MB, share_prompt=share)
+    ps.kv_paged_append()
+    if dt == "f8":
+        nb = B.paged_block_bytes(H, page, D, B.F8)
+        pools = [torch.zeros((n_blocks, nb), dtype=torch.uint8, device="cuda") for _ in range(2 * L)]
+        desc = ps.make_kv_pools_f8(pools[0::2], pools[1::2], H, D)
+    else:
+        pools = [torch.zeros((n_blocks, H, page, D), dtype=IO[dt], device="cuda") for _ in range(2 * L)]
+        desc = ps.make_kv_pools(pools[0::2], pools[1::2])
+    freqs, m = B.rope_frequencies(D, 10000.0, "yarn", 4.0, 1.0, 32.0, 64)
+    freqs = torch.from_numpy(freqs).cuda()
+    rope = B.Rope(freqs, "half", m)
+    mirror = torch.zeros((L, 2, R, H, ML, D), dtype=torch.float64, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda n, h: torch.randn((n, h, D), device="cuda", generator=g).to(IO[dt])
+
+    def stored(layer, rows, pos):
+        """What the cache holds at the positions just written (their contents are the business of the write tests)."""
+        t = ps.kv_paged_table
+        for w in range(2):
+            vals = PR.pool_values(pools[2 * layer + w], H, page, D)
+            mirror[layer, w, rows, :, pos] = vals[t[rows, pos // page].long(), :, pos % page]
+
+    # prompts: every row of a group holds the same, shared blocks are written through the group's first row
+    for layer in range(L):
+        for gi in range(G):
+            n = prompt[gi]
+            full = n // page * page if share else 0
+            k, v = rnd(n, H), rnd(n, H)
+            todo = [(gi * N, p) for p in range(full)] + [(gi * N + i, p) for i in range(N) for p in range(full, n)]
+            rows = torch.tensor([a for a, _ in todo], dtype=torch.int32, device="cuda")
+            pos = torch.tensor([b for _, b in todo], dtype=torch.int32, device="cuda")
+            ps.kv_paged_write(desc, layer, k[pos.long()], v[pos.long()], rope=rope, rows=rows, positions=pos)
+            everyone = torch.arange(gi * N, (gi + 1) * N, device="cuda").repeat_interleave(n)
+            stored(layer, everyone, torch.arange(n, device="cuda").repeat(N))
+
+    moved = 0
+    for t in range(1, T + 1):
+        lens, done = ps.lens, ps.done
+        live = torch.nonzero(done == 0).flatten()
+        if len(live) == 0:
+            break
+        for layer in range(L):
+            k, v, q = rnd(R, H), rnd(R, H), rnd(R, H * ratio)
+            qr = ps.kv_paged_write(desc, layer, k, v, q=q, rope=rope)
+            lc = live.cuda()
+            pos = lens.long().cuda()[lc]
+            stored(layer, lc, pos)
+            assert ((PR.rotate(k, lens.cuda(), freqs, "half", m)[lc] - mirror[layer, 0, lc, :, pos]).abs()
+                    <= 2.0 ** -4 * 1.02 * PR.rotate(k, lens.cuda(), freqs, "half", m)[lc].abs().amax(-1, keepdim=True)).all()
+            lse = torch.full((R, H * ratio), 7.0, device="cuda")
+            out = ps.kv_paged_attend(desc, layer, qr, D ** -0.5, lse=lse)
+            for r in range(R):
+                if done[r]:
+                    assert (out[r] == 0).all() and (lse[r] == 7.0).all()
+                    continue
+                n = int(lens[r]) + 1
+                want, wl, absv, reach = PR.attend(qr[r], mirror[layer, 0, r, :, :n], mirror[layer, 1, r, :, :n], D ** -0.5)
+                bound = PR.attend_bound(want, absv, reach, n, D, IO[dt], WEIGHT_STEP[dt])
+                assert ((out[r].double() - want).abs() <= bound).all()
+        ps.step(torch.randn((R, V), device="cuda", generator=g) * 3)
+        ps.reindex_kv_paged(desc)
+        move = ps.slot_map.view(G, N).long() + (torch.arange(G) * N)[:, None]
+        moved += ps.move_count
+        mirror = mirror[:, :, move.flatten().cuda()]
+        assert ps.sync_status() == B.OK
+    assert moved > 0
+    lens = ps.lens.tolist()
+    for layer in range(L):
+        dense = [torch.full((R, H, ML, D), 5.0, dtype=IO[dt], device="cuda") for _ in range(2)]
+        ps.kv_paged_read(desc, layer, dense[0], dense[1])
+        for w in range(2):
+            for r in range(R):
+                assert torch.equal(dense[w][r, :, :lens[r]].double(), mirror[layer, w, r, :, :lens[r]])
+                assert (dense[w][r, :, lens[r]:] == 5).all()
+    assert ps.sync_status() == B.OK
+    with pytest.raises(B.PsmcError):                     # a layer that the pools do not have
+        ps.kv_paged_read(desc, L, dense[0], dense[1])
+    ps.destroy()
+
+
+def test_the_context_forms_need_a_paged_cache():
+    ps = B.init_batched(1, 2, 16, 4.0, 0.25, 0.9, 0, 7, 1, T_max=4)
+    ps._paged = (4, 16, 2)
+    pools = ps.make_kv_pools([torch.zeros((4, 1, 16, 64), device="cuda")], [torch.zeros((4, 1, 16, 64), device="cuda")])
+    x = torch.zeros((2, 1, 64), device="cuda")
+    for call in (lambda: ps.kv_paged_write(pools, 0, x, x), lambda: ps.kv_paged_attend(pools, 0, x, 1.0),
+                 lambda: ps.kv_paged_read(pools, 0, torch.zeros((2, 1, 8, 64), device="cuda"))):
+        with pytest.raises(B.PsmcError) as e:
+            call()
+        assert e.value.code == B.E_STATE
+    ps.destroy()
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    c = Cache("bf16", [40, 17], 2, 64, 16, seed=8)
+    q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (q.float(), q[:1], q[:, :3], q[..., :32], q.transpose(1, 2), q.cpu()):
+        with pytest.raises(AssertionError):
+            B.paged_attend(c.handle, bad, c.lens, 1.0)
+    for bad in (c.lens.long(), c.lens[:1], c.lens.cpu()):
+        with pytest.raises(AssertionError):
+            B.paged_attend(c.handle, q, bad, 1.0)
+    with pytest.raises(AssertionError):
+        B.paged_attend(c.handle, q, c.lens, 1.0, scratch=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(AssertionError):
+        B.PagedKv(c.pools[0], c.pools[1][:1], c.table, 2, 64, 16)
+    with pytest.raises(AssertionError):
+        B.paged_read(c.handle, c.lens, torch.zeros((2, 2, 64, 40), dtype=torch.bfloat16, device="cuda").transpose(2, 3))

@@ -1,0 +1,154 @@
+"""The operators on the paged cache as far as no GPU is needed: refusals of bad arguments (made before anything is
+enqueued), the size of blocks, the scaled rotary frequencies against their formulas, and the 64-bit reference itself."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as PR
+
+
+@pytest.fixture(scope="module")
+def B():
+    import __graft_entry__ as entry
+    entry.build()
+    from paper_2602_10273_b200 import binding
+    binding.lib()
+    return binding
+
+
+def _kv(B, **over):
+    """A descriptor that would pass, with made-up addresses: a refused call never looks at them."""
+    f = dict(k=1 << 20, v=2 << 20, table=3 << 20, table_ld=4, R=2, n_blocks=8, block_len=16, max_blocks=4, n_kv_heads=2,
+             head_dim=64, dt=B.BF16)
+    f.update(over)
+    return B.PagedKvDesc(*[f[n] for n, _ in B.PagedKvDesc._fields_])
+
+
+BAD_KV = [dict(k=0), dict(v=0), dict(table=0), dict(table_ld=3), dict(R=0), dict(n_blocks=0), dict(block_len=0),
+          dict(max_blocks=0), dict(n_kv_heads=0), dict(head_dim=0), dict(head_dim=264), dict(head_dim=20),
+          dict(dt=3), dict(dt=-1), dict(k=(1 << 20) + 8), dict(v=(1 << 20) + 2), dict(table=(1 << 20) + 2),
+          dict(dt=2, head_dim=24), dict(dt=0, head_dim=3), dict(max_blocks=1 << 28, table_ld=1 << 28),
+          dict(block_len=1 << 25)]
+
+
+@pytest.mark.parametrize("bad", BAD_KV, ids=lambda d: ",".join("%s=%s" % i for i in d.items()))
+def test_a_bad_cache_is_refused_by_every_operator(B, bad):
+    L, kv, h = B.lib(), _kv(B, **bad), B.Heads(4 << 20, 128, 64)
+    r = C.byref
+    assert L.psmc_paged_write(r(kv), 1, 0, 1 << 20, 0, None, r(h), r(h), 0, None, None, 0, 0) == B.E_INVAL
+    assert L.psmc_paged_attend(r(kv), 1 << 20, 0, 0, 4, r(h), r(h), 1.0, 0, 1 << 20, 1 << 40, 0, 0) == B.E_INVAL
+    assert L.psmc_paged_read(r(kv), 1 << 20, 0, 1 << 20, 1 << 20, 16, 1 << 20, 1 << 12, 0, 0) == B.E_INVAL
+
+
+def test_bad_arguments_of_write_are_refused(B):
+    L, kv, h, r = B.lib(), _kv(B), B.Heads(4 << 20, 128, 64), C.byref
+    odd, none = B.Heads((4 << 20) + 1, 128, 64), B.Heads(0, 128, 64)
+    rope = B.RopeDesc(1 << 20, 64, 0, 1.0)
+
+    def call(kv_=None, n=1, rows=0, pos=1 << 20, rope_=None, k=r(h), v=r(h), Hq=4, q=r(h), q_out=r(h)):
+        return L.psmc_paged_write(r(kv) if kv_ is None else kv_, n, rows, pos, 0, rope_, k, v, Hq, q, q_out, 0, 0)
+
+    assert call(n=-1) == B.E_INVAL
+    assert call(n=3) == B.E_INVAL                       # rows NULL and more tokens than rows
+    assert call(pos=0) == B.E_INVAL
+    assert call(k=None) == call(v=None) == call(k=r(none)) == call(k=r(odd)) == call(q=r(odd)) == B.E_INVAL
+    assert call(q=None) == call(q_out=None) == B.E_INVAL  # one without the other
+    assert call(Hq=0) == B.E_INVAL
+    for bad in (B.RopeDesc(0, 64, 0, 1.0), B.RopeDesc(1 << 20, 63, 0, 1.0), B.RopeDesc(1 << 20, 0, 0, 1.0),
+                B.RopeDesc(1 << 20, 66, 0, 1.0), B.RopeDesc(1 << 20, 64, 2, 1.0)):
+        assert call(rope_=r(bad)) == B.E_INVAL
+    assert L.psmc_paged_write(None, 1, 0, 1 << 20, 0, r(rope), r(h), r(h), 0, None, None, 0, 0) == B.E_INVAL
+    assert call(n=0, rope_=r(rope)) == B.OK             # nothing to do: nothing is enqueued
+
+
+def test_bad_arguments_of_attend_and_read_are_refused(B):
+    L, kv, h, r = B.lib(), _kv(B), B.Heads(4 << 20, 128, 64), C.byref
+    need = L.psmc_paged_attend_scratch_bytes(2, 4, 2, 64)
+
+    def attend(lens=1 << 20, extra=0, Hq=4, q=r(h), out=r(h), scratch=1 << 20, nbytes=need):
+        return L.psmc_paged_attend(r(kv), lens, extra, 0, Hq, q, out, 1.0, 0, scratch, nbytes, 0, 0)
+
+    assert need > 0
+    assert attend(lens=0) == attend(extra=-1) == attend(Hq=0) == attend(Hq=3) == attend(q=None) == attend(out=None) == B.E_INVAL
+    assert attend(scratch=0) == attend(scratch=(1 << 20) + 16) == attend(nbytes=need - 1) == B.E_INVAL
+    for bad in ((0, 4, 2, 64), (2, 0, 2, 64), (2, 3, 2, 64), (2, 4, 0, 64), (2, 4, 2, 0), (2, 4, 2, 257)):
+        assert L.psmc_paged_attend_scratch_bytes(*bad) == 0
+
+    def read(lens=1 << 20, k=1 << 20, v=1 << 20, max_len=16, row=2048, head=1024):
+        return L.psmc_paged_read(r(kv), lens, 0, k, v, max_len, row, head, 0, 0)
+
+    assert read(lens=0) == read(k=0, v=0) == read(max_len=0) == read(row=2047) == read(head=1023) == read(k=(1 << 20) + 1) == B.E_INVAL
+
+
+def test_the_context_forms_refuse_without_a_context(B):
+    L, h, r = B.lib(), B.Heads(4 << 20, 128, 64), C.byref
+    assert L.psmc_kv_paged_write(None, None, 0, 1, 0, 0, None, r(h), r(h), 0, None, None, 0) == B.E_INVAL
+    assert L.psmc_kv_paged_attend(None, None, 0, 4, r(h), r(h), 1.0, 0, 1 << 20, 1 << 40, 0) == B.E_INVAL
+    assert L.psmc_kv_paged_read(None, None, 0, 1 << 20, 1 << 20, 16, 2048, 1024, 0) == B.E_INVAL
+
+
+def test_block_bytes(B):
+    assert B.paged_block_bytes(8, 16, 128, B.BF16) == 8 * 16 * 128 * 2
+    assert B.paged_block_bytes(2, 16, 64, B.F32) == 2 * 16 * 64 * 4
+    assert B.paged_block_bytes(8, 16, 128, B.F8) == 8 * 16 * 128 + 128
+    assert B.paged_block_bytes(3, 7, 16, B.F8) == 3 * 7 * 16 + 32          # 21 scale bytes, padded
+    assert B.paged_block_bytes(0, 16, 128, B.BF16) == B.paged_block_bytes(8, 16, 128, 3) == 0
+
+
+@pytest.mark.parametrize("rot", [2, 6, 64, 128])
+def test_rotary_frequencies(B, rot):
+    theta, s, T = 10000.0, 8.0, 4096
+    base = np.array([theta ** (-2.0 * j / rot) for j in range(rot // 2)])
+    f, m = B.rope_frequencies(rot, theta)
+    np.testing.assert_allclose(f, base, rtol=1e-14)
+    assert m == 1.0
+    f, m = B.rope_frequencies(rot, theta, "linear", s)
+    np.testing.assert_allclose(f, base / s, rtol=1e-14)
+    if rot > 2:
+        f, m = B.rope_frequencies(rot, theta, "base", s)
+        np.testing.assert_allclose(f, [(theta * s ** (rot / (rot - 2))) ** (-2.0 * j / rot) for j in range(rot // 2)], rtol=1e-13)
+        assert abs(f[-1] * s - base[-1]) < 1e-12 * base[-1]   # the slowest pair ends up divided by the factor
+    f, m = B.rope_frequencies(rot, theta, "bands", s, 1.0, 4.0, T)
+    for got, w in zip(f, base):
+        turns = T * w / (2 * math.pi)
+        want = w if turns >= 4 else w / s if turns <= 1 else ((turns - 1) * w + (4 - turns) * w / s) / 3
+        assert abs(got - want) <= 1e-14 * want
+    f, m = B.rope_frequencies(rot, theta, "yarn", s, 1.0, 32.0, T)
+    assert abs(m - (0.1 * math.log(s) + 1)) < 1e-15
+    lo = max(0, math.floor(rot * math.log(T / (64 * math.pi)) / (2 * math.log(theta))))
+    hi = min(rot - 1, math.ceil(rot * math.log(T / (2 * math.pi)) / (2 * math.log(theta))))
+    for j, (got, w) in enumerate(zip(f, base)):
+        slow = min(1.0, max(0.0, (j - lo) / max(hi - lo, 0.001)))
+        assert abs(got - (w * (1 - slow) + w / s * slow)) <= 1e-14 * w
+
+
+def test_rotary_frequencies_refuse(B):
+    out = np.empty(64)
+    call = lambda kind=0, rot=64, theta=1e4, s=2.0, lo=1.0, hi=4.0, T=100, p=out.ctypes.data: B.lib().psmc_rope_frequencies(
+        kind, rot, theta, s, lo, hi, T, p, None)
+    assert call() == B.OK
+    assert call(kind=5) == call(kind=-1) == call(rot=0) == call(rot=7) == call(theta=1.0) == call(s=0.5) == call(p=None) == B.E_INVAL
+    assert call(kind=2, rot=2) == call(kind=3, lo=0.0) == call(kind=3, hi=1.0) == call(kind=4, T=0) == B.E_INVAL
+    assert call(theta=math.nan) == call(s=math.nan) == B.E_INVAL
+    assert call(kind=0, lo=0.0, hi=0.0, T=0) == B.OK     # not read
+
+
+def test_the_reference_quantiser_and_codes():
+    codes = torch.arange(256, dtype=torch.uint8)
+    want = codes.view(torch.float8_e4m3fn).double()
+    got = PR.code_values(codes)
+    assert torch.equal(got.nan_to_num(9e9), want.nan_to_num(9e9))
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(200, 64, generator=g, dtype=torch.float64) * torch.exp2(torch.randint(-20, 20, (200, 1), generator=g).double())
+    x[0], x[1, :] = 0, 448.0
+    e, q = PR.quantise(x)
+    s = torch.ldexp(torch.ones_like(x), e[:, None].expand_as(x))
+    assert e[0] == -60 and e[1] == 0
+    assert ((x.abs() / s).amax(-1)[1:] <= 448).all() and ((x.abs() / s).amax(-1)[1:] > 224).all()
+    near = ((x / s).float().to(torch.float8_e4m3fn)).double() * s
+    assert ((near - q).abs() <= 1e-6 * s).all()          # float first: equal but where a double rounding decides a tie
+    tiny = s * 2.0 ** -9
+    assert ((q - x).abs() <= torch.maximum(x.abs() * 2.0 ** -4, tiny / 2)).all()
