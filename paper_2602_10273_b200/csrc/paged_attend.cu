@@ -21,6 +21,9 @@
 // instructions reach a fraction of the tensor cores' rate, and a fraction is enough: at 4 queries per head the arithmetic
 // of a step is 1/10 of the time its bytes take.)  A weight is exp2(s - m) with m a reference per query that follows the
 // largest score only when it is exceeded by more than 8 (a rare, warp-uniform branch); sums and outputs are fp32.
+#include <cuda.h>
+
+#include "bulk_copy.cuh"
 #include "paged_common.cuh"
 
 namespace psmc {
@@ -34,16 +37,16 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;       // how far (log2) a score may exceed the reference before the reference moves
 
 // ---------------------------------------------------------------------------------------------------------- plan
-struct Segment {
+struct alignas(16) Segment {
     uint32_t mask;       // rows of the tile
     int p0, p1;          // positions
     int before;          // rows of the segments before this one, added up
     int64_t start;       // its first cost unit on the line of one (tile, key-value head)
 };
-struct TilePlan {
-    int64_t cost;        // of one key-value head
+struct alignas(16) TilePlan {
     int n_segs;
     uint32_t whole;      // rows that have a single segment
+    int64_t cost;        // of one key-value head
     uint32_t left_out;   // rows with skip != 0, or beyond R
     Segment seg[kMaxSegs];
 };
@@ -54,13 +57,13 @@ struct LineShape {       // how the items of a tile are cut; a pure function of 
     int ratio, H;
 };
 // What a step costs by its queries: its bytes are the same, and beside them the arithmetic of one or two groups is small.
-__device__ __forceinline__ int step_cost(const LineShape& s, int nq) {
-    const int groups = (nq + s.group - 1) / s.group;
+__device__ __forceinline__ int step_cost(int group, int nq) {
+    const int groups = (nq + group - 1) / group;
     return 4 + (groups > 1 ? groups : 0);
 }
 __device__ __forceinline__ int64_t seg_cost(const LineShape& s, int rows, int steps) {
     const int nq = rows * s.ratio, qt = s.group * kGroups, full = nq / qt, rem = nq - full * qt;
-    return (int64_t)steps * (full * step_cost(s, qt) + (rem ? step_cost(s, rem) : 0));
+    return (int64_t)steps * (full * step_cost(s.group, qt) + (rem ? step_cost(s.group, rem) : 0));
 }
 __device__ __forceinline__ int steps_of(const LineShape& s, int p0, int p1) { return (p1 - p0 + s.step - 1) / s.step; }
 
@@ -108,29 +111,43 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
 
     // How this row stands in block j: positions of it that count, and the block's number, if it has one that exists.
     const auto live_in = [&](int j) -> int { return (int)min((int64_t)B, max((int64_t)0, n - (int64_t)j * B)); };
-    const auto set_of = [&](int entry, int live) -> uint32_t {  // rows that stand alike, this one among them
-        const bool named = live > 0 && entry >= 0 && entry < c.n_blocks;
-        const uint32_t same = __match_any_sync(kFull, named ? entry : -1 - lane) & __match_any_sync(kFull, live);
-        return live > 0 ? (named ? same : 1u << lane) : 0u;
+    const auto name_of = [&](int entry, int live) -> int { return live > 0 && entry >= 0 && entry < c.n_blocks ? entry : -1 - lane; };
+    // rows that stand alike in a block, this one among them (0: the row ends before it)
+    const auto all_like = [&](int name, int live) -> uint32_t {
+        const uint32_t same = __match_any_sync(kFull, name);
+        const uint32_t alike = __any_sync(kFull, live != __shfl_sync(kFull, live, __ffs(same) - 1)) ? __match_any_sync(kFull, live) : kFull;
+        return live > 0 ? same & alike : 0u;
     };
     int begun = 0, rows = 0;
     if (__popc(alive) > 1) {
         for (int j0 = warp * kRun; j0 < nb; j0 += kPlanWarps * kRun) {
             if (j0 >= kPlanWarps * kRun) fetch(j0);
-            uint32_t prev = 0;
-            if (j0 > 0) prev = set_of(e[0], live_in(j0 - 1));
+            uint32_t set = 0;
+            if (j0 > 0) set = all_like(name_of(e[0], live_in(j0 - 1)), live_in(j0 - 1));
+            else set = alive;  // before the first block all rows are one set; block 0 begins a segment in any case
 #pragma unroll
             for (int u = 0; u < kRun; ++u) {
-                const int j = j0 + u, live = live_in(j);
+                const int j = j0 + u, live = live_in(j), name = name_of(e[u + 1], live);
                 if (j >= nb) break;
-                // A match over the warp costs hundreds of cycles when the rows differ.  Where every row still stands like
-                // the first of its set, no set has split, and sets that have once parted do not meet again in a table that
-                // copy-on-write keeps (in any other table two sets would just be read apart).
-                const int lead = prev ? __ffs(prev) - 1 : lane;
-                const int lead_e = __shfl_sync(kFull, e[u + 1], lead), lead_live = __shfl_sync(kFull, live, lead);
-                uint32_t set = prev;
-                if (__any_sync(kFull, (prev == 0) != (live == 0) || lead_live != live || (prev != 0 && lead_e != e[u + 1])))
-                    set = set_of(e[u + 1], live);
+                // Sets only ever split: copy-on-write keeps two rows apart once they have parted, and in any other table
+                // two sets that meet again are just read apart.  A set splits where some row of it does not stand like its
+                // first row; its pieces are taken off one by one, first rows first.
+                const uint32_t prev = j == 0 ? 0u : set;
+                uint32_t open = __ballot_sync(kFull, set != 0), mine = set;
+                if (live == 0) set = 0;
+                for (int piece = 0; open && piece < kTileRows; ++piece) {
+                    const int lead = mine ? __ffs(mine) - 1 : lane;
+                    const int lead_name = __shfl_sync(kFull, name, lead), lead_live = __shfl_sync(kFull, live, lead);
+                    const bool like = name == lead_name && live == lead_live;
+                    const uint32_t alike = __ballot_sync(kFull, mine != 0 && like);
+                    if (mine != 0 && like) {
+                        if (live > 0) set = mine & alike;
+                        mine = 0;
+                    } else {
+                        mine &= ~alike;
+                    }
+                    open = __ballot_sync(kFull, mine != 0);
+                }
                 const bool begins = set != 0 && set != prev && lane == __ffs(set) - 1;
                 const uint32_t who = __ballot_sync(kFull, begins);
                 if (begins) {
@@ -139,7 +156,6 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
                     if (s < kWarpSegs) found[warp][s] = Found{set, j, lane};
                 }
                 begun += __popc(who);
-                prev = set;
             }
         }
     }
@@ -184,7 +200,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
             const int64_t cs_upto = warp_scan_incl<long long>(cs, lane);
             const int held_upto = warp_scan_incl(held, lane);
             if (in) {
-                tp.seg[s] = Segment{f.mask, p0, p1, before + held_upto - held, cost + cs_upto - cs};
+                tp.seg[s] = Segment{f.mask, p0, p1, before + held_upto - held, cost + (cs_upto - cs)};
                 bool all = p0 == 0;  // every row of the set ends where the segment does
                 for (uint32_t m = f.mask; m && all; m &= m - 1) all = n_of[__ffs(m) - 1] == p1;
                 if (all) whole |= f.mask;
@@ -216,16 +232,22 @@ struct Bearings {        // where a tile begins on the line, and how the line is
     int64_t before, share, total;
     int tile;
 };
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {  // x >= 0, y > 0; nearly always small
+    if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
+    return x / y;
+}
 // The tile that holds cost unit `worker * share` (or the one asked for), by all lanes of a warp: the costs of all tiles are
 // added up again (16 numbers for 512 rows), which is less than a kernel of its own would take.
 __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile, int lane) {
-    int64_t sum = 0;
-    for (int t = lane; t < l.n_tiles; t += 32) sum += l.plans[t].cost;
+    const auto cost_of = [&](int t) -> int64_t { return t < l.n_tiles ? l.plans[t].cost * l.ls.H : 0; };
+    const int64_t head_cs = cost_of(lane);  // all of them, for up to 1024 rows
+    int64_t sum = head_cs;
+    for (int t = lane + 32; t < l.n_tiles; t += 32) sum += cost_of(t);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, (long long)sum, o);
     Bearings b;
-    b.total = sum * l.ls.H;
-    b.share = (b.total + l.workers - 1) / l.workers;
+    b.total = sum;
+    b.share = quotient(b.total + l.workers - 1, l.workers);
     if (b.share < 4) b.share = 4;  // one step
     const int64_t x = worker * b.share;
     int64_t base = 0;
@@ -233,7 +255,7 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
     b.before = b.total;
     for (int t0 = 0; t0 < l.n_tiles; t0 += 32) {
         const int t = t0 + lane;
-        const int64_t cs = t < l.n_tiles ? l.plans[t].cost * l.ls.H : 0;
+        const int64_t cs = t0 == 0 ? head_cs : cost_of(t);
         const int64_t upto = base + warp_scan_incl<long long>(cs, lane);
         const uint32_t hit = __ballot_sync(kFull, t < l.n_tiles && (tile >= 0 ? t == tile : upto > x));
         if (hit) {
@@ -253,11 +275,21 @@ __device__ __forceinline__ int steps_before(int64_t bound, int64_t a, int w, int
     return d >= (int64_t)steps * w ? steps : (int)(((uint32_t)d + (uint32_t)w - 1) / (uint32_t)w);
 }
 
+// What the arithmetic of an item has to know of it; the copying side, which is ahead, leaves it in a queue.
+struct alignas(16) Item {
+    uint32_t mask;
+    int tile, head, qt;
+    int nq, steps, p0;   // queries of this query tile; steps that are this worker's; the position at which they begin
+    int alone;           // the whole of its rows, in this share
+    int64_t slot;        // where the partial result of its query 0 goes
+};
+
 // One worker's walk along the line.  All threads of the CTA hold the same values.
+template <class S>
 struct Walk {
     int64_t a, hi;       // first cost unit of the item at hand; end of the share
     int tile, head, si, qt, n_qt, n_segs;
-    uint32_t mask;
+    uint32_t mask, whole;
     int p0, p1;          // positions of the segment
     int nq;              // queries of this query tile
     int before;          // see Segment
@@ -265,19 +297,31 @@ struct Walk {
     int s, s_end;        // steps of the item that are this worker's: the next one, and the end
     int s_first;
     bool done;
+    int4 next_seg;       // the segment after this one (asked for when this one is entered), and its tile's first words
+    int2 next_tile;
 
-    __device__ __forceinline__ void open_segment(const Line& l) {
-        const Segment& g = l.plans[tile].seg[si];
-        mask = g.mask;
-        p0 = g.p0;
-        p1 = g.p1;
-        before = g.before;
-        steps = steps_of(l.ls, p0, p1);
-        n_qt = (__popc(mask) * l.ls.ratio + kGroups * l.ls.group - 1) / (kGroups * l.ls.group);
+    __device__ __forceinline__ void look_ahead(const Line& l) {
+        int t = tile, n = si + 1;
+        if (n >= n_segs) {
+            n = 0;
+            if (head + 1 >= l.ls.H) ++t;
+        }
+        if (t >= l.n_tiles) return;
+        next_seg = *reinterpret_cast<const int4*>(&l.plans[t].seg[n]);
+        if (t != tile) next_tile = *reinterpret_cast<const int2*>(&l.plans[t]);
     }
-    __device__ __forceinline__ void open_item(const Line& l, int64_t lo) {
-        nq = min(kGroups * l.ls.group, __popc(mask) * l.ls.ratio - qt * kGroups * l.ls.group);
-        w = step_cost(l.ls, nq);
+    __device__ __forceinline__ void enter_segment(const Line& l, const int4& g) {
+        mask = (uint32_t)g.x;
+        p0 = g.y;
+        p1 = g.z;
+        before = g.w;
+        steps = (p1 - p0 + S::kStep - 1) / S::kStep;
+        n_qt = (__popc(mask) * l.ls.ratio + kGroups * S::kGroup - 1) / (kGroups * S::kGroup);
+        look_ahead(l);
+    }
+    __device__ __forceinline__ void enter_item(const Line& l, int64_t lo) {
+        nq = min(kGroups * S::kGroup, __popc(mask) * l.ls.ratio - qt * kGroups * S::kGroup);
+        w = step_cost(S::kGroup, nq);
         s_first = s = steps_before(lo, a, w, steps);
         s_end = steps_before(hi, a, w, steps);
     }
@@ -291,25 +335,40 @@ struct Walk {
             }
             if (++qt >= n_qt) {
                 qt = 0;
+                int4 g = next_seg;
                 if (++si >= n_segs) {
                     si = 0;
                     if (++head >= l.ls.H) {
                         head = 0;
-                        do {
-                            if (++tile >= l.n_tiles) {
-                                done = true;
-                                return;
-                            }
-                            n_segs = l.plans[tile].n_segs;
-                        } while (n_segs == 0);
+                        if (++tile >= l.n_tiles) {
+                            done = true;
+                            return;
+                        }
+                        n_segs = next_tile.x;
+                        whole = (uint32_t)next_tile.y;
+                        if (n_segs == 0) {  // tiles without any position
+                            do {
+                                if (++tile >= l.n_tiles) {
+                                    done = true;
+                                    return;
+                                }
+                                n_segs = l.plans[tile].n_segs;
+                            } while (n_segs == 0);
+                            whole = l.plans[tile].whole;
+                            g = *reinterpret_cast<const int4*>(&l.plans[tile].seg[0]);
+                        }
                     }
                 }
-                open_segment(l);
+                enter_segment(l, g);
             }
-            open_item(l, a);
+            enter_item(l, a);
         } while (s >= s_end);
     }
     __device__ __forceinline__ void begin(const Line& l, int worker, int lane) {
+        // the first tile's segments are asked for before it is known which tile it is: of up to 32 rows there is one
+        int4 seg = *reinterpret_cast<const int4*>(&l.plans[0].seg[lane]);
+        int64_t start = l.plans[0].seg[lane].start;
+        int2 head_words = *reinterpret_cast<const int2*>(&l.plans[0]);
         const Bearings b = bearings(l, worker, -1, lane);
         const int64_t lo = worker * b.share;
         hi = min(lo + b.share, b.total);
@@ -317,36 +376,53 @@ struct Walk {
         if (done) return;
         tile = b.tile;
         const TilePlan& tp = l.plans[tile];
-        n_segs = tp.n_segs;
-        const int64_t x = lo - b.before;
-        int64_t start[kMaxSegs / 32];
-#pragma unroll
-        for (int i = 0; i < kMaxSegs / 32; ++i) start[i] = tp.seg[i * 32 + lane].start;  // those beyond n_segs are not looked at
-        head = (int)(x / tp.cost);
-        const int64_t y = x - head * tp.cost;
+        if (tile != 0) {
+            seg = *reinterpret_cast<const int4*>(&tp.seg[lane]);
+            start = tp.seg[lane].start;
+            head_words = *reinterpret_cast<const int2*>(&tp);
+        }
+        const int64_t cost = tp.cost, x = lo - b.before;
+        n_segs = head_words.x;
+        whole = (uint32_t)head_words.y;
+        head = (int)quotient(x, cost);
+        const int64_t y = x - head * cost;
         si = -1;
-#pragma unroll
-        for (int i = 0; i < kMaxSegs / 32; ++i) si += __popc(__ballot_sync(kFull, i * 32 + lane < n_segs && start[i] <= y));
-        int64_t first = start[0];
-#pragma unroll
-        for (int i = 1; i < kMaxSegs / 32; ++i)
-            if (si >= i * 32) first = start[i];
-        first = __shfl_sync(kFull, (long long)first, si & 31);
-        open_segment(l);
-        const int64_t full = (int64_t)steps * step_cost(l.ls, kGroups * l.ls.group);
-        qt = (int)min((int64_t)(n_qt - 1), (y - first) / full);
-        a = b.before + head * tp.cost + first + qt * full;
-        open_item(l, lo);
+        int4 g = seg;
+        int64_t first = 0;
+        for (int s0 = 0;;) {
+            const int upto = __popc(__ballot_sync(kFull, s0 + lane < n_segs && start <= y));
+            if (upto > 0) {
+                si = s0 + upto - 1;
+                g = int4{__shfl_sync(kFull, seg.x, upto - 1), __shfl_sync(kFull, seg.y, upto - 1), __shfl_sync(kFull, seg.z, upto - 1),
+                         __shfl_sync(kFull, seg.w, upto - 1)};
+                first = __shfl_sync(kFull, (long long)start, upto - 1);
+            }
+            s0 += 32;
+            if (upto < 32 || s0 >= n_segs) break;
+            seg = *reinterpret_cast<const int4*>(&tp.seg[s0 + lane]);
+            start = tp.seg[s0 + lane].start;
+        }
+        enter_segment(l, g);
+        const int64_t full = (int64_t)steps * step_cost(S::kGroup, kGroups * S::kGroup);
+        qt = (int)min((int64_t)(n_qt - 1), quotient(y - first, full));
+        a = b.before + head * cost + first + qt * full;
+        enter_item(l, lo);
         if (s >= s_end) next_item(l);
     }
-    __device__ __forceinline__ bool alone(const Line& l) const {  // the whole of its rows, in this share
-        return s_first == 0 && s_end == steps && (l.plans[tile].whole & mask) == mask;
-    }
-    // where the partial result of the item's query 0 goes
-    __device__ __forceinline__ int64_t slot(const Line& l, int worker) const {
-        const int in_tile = qt * kGroups * l.ls.group;
-        if (s_first > 0) return l.first_rest + (int64_t)worker * (kGroups * l.ls.group);
-        return ((int64_t)tile * l.ls.H + head) * (kTileRows * kRowSegs * l.ls.ratio) + (int64_t)before * l.ls.ratio + in_tile;
+    __device__ __forceinline__ Item item(const Line& l, int worker) const {
+        Item it;
+        it.mask = mask;
+        it.tile = tile;
+        it.head = head;
+        it.qt = qt;
+        it.nq = nq;
+        it.steps = s_end - s;
+        it.p0 = p0 + s * S::kStep;
+        it.alone = s_first == 0 && s_end == steps && (whole & mask) == mask;
+        it.slot = s_first > 0 ? l.first_rest + (int64_t)worker * (kGroups * S::kGroup)
+                              : ((int64_t)tile * l.ls.H + head) * (kTileRows * kRowSegs * l.ls.ratio) + (int64_t)before * l.ls.ratio +
+                                    qt * kGroups * S::kGroup;
+        return it;
     }
 };
 
@@ -367,8 +443,8 @@ __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -420,28 +496,37 @@ __device__ __forceinline__ uint32_t codes_to_f16(uint32_t x) {
 }
 
 // Shape of a CTA's work.  DP: head_dim rounded up to what the tiles are unrolled for.
+// A stage holds the keys of a step, then its values: panels of 128 bytes of every position's row, a row's 16-byte units
+// exchanged among themselves by the row's number (unit u of row r lies at u ^ (r % 8)), so that the 8 rows an operand load
+// touches lie in different banks.  That is what tiled bulk copies write with 128-byte swizzling.
 constexpr int kWarps = 4;
+constexpr int kPanel = 128;
 template <int DT_, int DP_>
 struct Shape {
     static constexpr int DT = DT_, DP = DP_;
     static constexpr int kElem = DT == PSMC_F32 ? 4 : (DT == PSMC_BF16 ? 2 : 1);
-    static constexpr int kRow = DP * kElem + 16;                          // bytes between rows: an odd number of 16-byte units
-    static constexpr int kStep = DT == PSMC_F32 && DP > 128 ? 32 : 64;    // positions per step
+    static constexpr int kPanels = (DP * kElem + kPanel - 1) / kPanel;
+    static constexpr int kStep = DT == PSMC_F32 && DP > 128 ? 32 : (DT == PSMC_F8 && DP <= 128 ? 128 : 64);  // positions
     static constexpr int kSlices = kStep / 16;                            // the 16 positions of an operand tile
-    static constexpr int kHalf = kStep * kRow;                            // keys, then values
-    static constexpr int kScales = DT == PSMC_F8 ? kStep * 4 : 0;         // words that hold the scale bytes
-    static constexpr int kStage = 2 * (kHalf + kScales);
+    static constexpr int kPair = kSlices > kWarps ? 2 : 1;                // slices that a warp takes at a time
+    static constexpr int kHalf = kStep * kPanel * kPanels;                // keys, then values
+    static constexpr int kScales = DT == PSMC_F8 ? kStep : 0;             // scale bytes
+    static constexpr int kStage = (2 * (kHalf + kScales) + 1023) / 1024 * 1024;
     static constexpr int kGroup = DT == PSMC_F32 ? 8 : 16;                // queries per warp
     // 32-bit caches: queries [8][DP] and weights [16 positions][8 queries] of each warp
     static constexpr int kExtra = DT == PSMC_F32 ? kWarps * (8 * DP + 16 * 8) * 4 : 0;
-    static constexpr int kCtas = 3 * kStage + kExtra <= 112 * 1024 ? 2 : 1;  // per SM
-    static constexpr int kFit = (224 * 1024 / kCtas - kExtra) / kStage;
+    // shared memory of one CTA: half of an SM's 228 KB, or the 227 KB that one may have, less 1 KB that the system keeps of
+    // each, 1 KB for the ring's alignment and what lies beside the ring
+    static constexpr int kBeside = 2100, kHalfSm = 114 * 1024 - 2048 - kBeside, kWholeSm = 227 * 1024 - 1024 - kBeside;
+    static constexpr int kCtas = 3 * kStage + kExtra <= kHalfSm ? 2 : 1;  // per SM
+    static constexpr int kFit = ((kCtas == 2 ? kHalfSm : kWholeSm) - kExtra) / kStage;
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
-    static constexpr int kBytes = kStages * kStage + kExtra;
-    static_assert(kStages >= 2 && kStage >= 3 * 8 * DP * 4, "a ring; a stage holds the merge of one query tile");
+    static constexpr int kBytes = kStages * kStage + kExtra + 1024;
+    static_assert(kStages >= (DT == PSMC_F8 ? 3 : 2) && kStage >= kWarps * 8 * (DP + 4) * 4, "a ring; a stage holds the warps' outputs of a query tile");
 };
 
 struct AttendArgs {
+    CUtensorMap k_map, v_map;  // pools as [block][head, position][component], for tiled copies
     PagedView c;
     PagedAttend a;
     Line l;
@@ -449,81 +534,184 @@ struct AttendArgs {
     int q_words;         // queries start on 4-byte boundaries throughout
 };
 
-// The copying side of a walk.  Warp w copies the step's positions w*16 .. (the CTA's warps share them evenly); what a copy
-// needs from the block table is asked for two steps before it is issued.
+__device__ __forceinline__ void tiled_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// The copying side of a walk.  Warp w copies a quarter of a step's positions; what a copy needs from the block table is
+// asked for two steps before it is issued.  Items are put into the queue when their first step is asked for, so they are
+// there, with a barrier in between, before their first step is worked on; the queue is longer than this side is ahead.
+//
+// TILED: blocks are multiples of 16 positions, so 16 positions of one head lie in one block and travel as one tiled bulk copy
+// per panel (and a 16-byte one for their scales): a few instructions per step, where 16 bytes per lane and copy took the
+// load path 700 to 2000 cycles of each step.  Other block lengths are copied that way, a position wherever it lies.
+constexpr int kQueue = 16;
+
 template <class S>
+struct Shared {          // beside the ring
+    uint64_t full[S::kStages];           // TILED: a stage's copies have landed
+    uint32_t valid[S::kStages][S::kSlices];  // which of a slice's 16 positions hold something
+    int entries[4][S::kSlices];          // TILED: table entries of the steps asked for
+    Item queue[kQueue];
+    uint8_t rows[2][kWarps][kTileRows];  // row lists of this item and the next
+    float2 stats[kWarps][16];            // {reference, sum} of each warp's queries
+    float scaled[kWarps][16];            // its sum as a share of the largest reference of the query's slices
+};
+
+struct Pipe {            // the ring of stages as a CTA sees it
+    char* ring;
+    uint32_t ring_at;
+    int stage;           // the stage of the next step to be worked on
+    uint32_t phase;      // TILED: its barrier's
+    int worker, warp, lane;
+};
+
+template <class S, bool TILED>
 struct Feeder {
-    static constexpr int kMine = S::kStep / kWarps;  // positions per warp
+    static constexpr int kMine = S::kStep / kWarps;     // positions per warp
+    static constexpr int kUnits = TILED ? (kMine + 15) / 16 : kMine;  // what a lane asks for: a slice, or a position
+    static constexpr int kSpan = TILED ? 16 : 1;
     struct Asked {
-        int entry;       // lane p: table entry of the warp's position p
-        int in_block;    // lane p: head * block_len + offset in the block; -1: no such position
+        int entry;       // lane u: table entry of the warp's unit u (TILED: of the step in the ring of entries)
+        int in_block;    // lane u: head * block_len + offset in the block
+        int live;        // lane u: positions of it that lie in the segment
         bool any;        // whether there is a step at all
     };
-    Walk walk;
+    Walk<S> walk;
     Asked first, second;
+    int items;           // put into the queue so far
+    int asked;           // steps asked for so far
+    int scales, scales_at;  // not TILED, 8-bit: scale bytes on their way to a stage
 
-    __device__ __forceinline__ Asked ask(const AttendArgs& g, int warp, int lane) {
-        Asked q{-1, -1, !walk.done};
-        if (walk.done) return q;
-        const int p = walk.p0 + walk.s * S::kStep + warp * kMine + lane;
-        if (lane < kMine && p < walk.p1) {
-            const int j = div_by(p, g.by_block);
-            q.in_block = walk.head * g.c.block_len + (p - j * g.c.block_len);
-            const int row = walk.tile * kTileRows + __ffs(walk.mask) - 1;
-            q.entry = __ldg(g.c.table + (int64_t)row * g.c.table_ld + j);
+    // TILED: the slice a lane sees to; steps of 32 have two, and the even warps copy one each
+    static __device__ __forceinline__ int slice_of(const Pipe& pp) { return S::kSlices >= kWarps ? pp.warp * kUnits + pp.lane : pp.warp / 2; }
+    __device__ __forceinline__ Asked ask(const AttendArgs& g, const Pipe& pp, Shared<S>& sh) {
+        Asked q{-1, 0, 0, !walk.done};
+        if (walk.done) {
+            if (TILED) copies_commit();
+            ++asked;
+            return q;
         }
+        if (walk.s == walk.s_first) {
+            if (pp.warp == 0 && pp.lane == 0) sh.queue[items % kQueue] = walk.item(g.l, pp.worker);
+            ++items;
+        }
+        const int p = walk.p0 + walk.s * S::kStep + pp.warp * kMine + pp.lane * kSpan;
+        if (pp.lane < kUnits && p < walk.p1 && (S::kSlices >= kWarps || !TILED || pp.warp % 2 == 0)) {
+            const int j = div_by(p, g.by_block), row = walk.tile * kTileRows + __ffs(walk.mask) - 1;
+            const int32_t* from = g.c.table + (int64_t)row * g.c.table_ld + j;
+            q.in_block = walk.head * g.c.block_len + (p - j * g.c.block_len);
+            q.live = min(kSpan, walk.p1 - p);
+            // an asynchronous copy, where a load's result would be waited for as soon as it is passed on in a register
+            if (TILED) copy4(smem_of(&sh.entries[asked % 4][slice_of(pp)]), from);
+            else q.entry = __ldg(from);
+        }
+        if (TILED) copies_commit();
+        ++asked;
         if (++walk.s >= walk.s_end) walk.next_item(g.l);
         return q;
     }
-    __device__ __forceinline__ void begin(const AttendArgs& g, int warp, int lane) {
-        first = ask(g, warp, lane);
-        second = ask(g, warp, lane);
-    }
-    // copies of the step asked for first, into the stage at `stage`; valid_out: which of the warp's positions hold something
-    __device__ __forceinline__ void issue(const AttendArgs& g, uint32_t stage, uint32_t* valid_out, int warp, int lane) {
+    // copies of the step asked for first, into stage `to`
+    __device__ __forceinline__ void issue(const AttendArgs& g, int to, const Pipe& pp, Shared<S>& sh) {
+        const uint32_t stage = pp.ring_at + to * S::kStage;
+        const int warp = pp.warp, lane = pp.lane;
+        if (!TILED && S::DT == PSMC_F8) put_scales(pp);
         if (first.any) {
-            const bool named = first.in_block >= 0 && first.entry >= 0 && first.entry < g.c.n_blocks;
-            if (first.in_block >= 0 && !named) raise_status(g.a.status, PSMC_E_STATE);
-            const uint32_t valid = __ballot_sync(kFull, named);
-            const int per_row = g.c.D * S::kElem / 16;
-            const uint32_t unit =
-                named ? (uint32_t)first.entry * (uint32_t)(g.c.blk_bytes / 16) + (uint32_t)(first.in_block * per_row) : 0u;
-            constexpr int kPerRow = S::DP * S::kElem / 16, kCopies = kMine * kPerRow / 32;
-            const uint32_t to = stage + warp * kMine * S::kRow;
+            if (TILED) {
+                copies_wait<1>();  // the entries asked for last may still be on their way
+                if (first.live > 0) first.entry = sh.entries[(asked - 2) % 4][slice_of(pp)];
+            }
+            const bool named = first.live > 0 && first.entry >= 0 && first.entry < g.c.n_blocks;
+            if (first.live > 0 && !named) raise_status(g.a.status, PSMC_E_STATE);
+            if (TILED) {
+                const int slice = slice_of(pp);
+                const bool owner = lane < kUnits && (S::kSlices >= kWarps || warp % 2 == 0);
+                if (owner) sh.valid[to][slice] = named ? (1u << first.live) - 1u : 0u;
+                const int copies = __popc(__ballot_sync(kFull, owner && named));
+                if (lane == 0) mbar_expect_tx(&sh.full[to], copies * (2 * S::kPanels * 16 * kPanel + (S::DT == PSMC_F8 ? 32 : 0)));
+                __syncwarp();
+                if (owner && named) {
+                    const uint32_t dst = stage + slice * 16 * kPanel;
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const int x = i * 32 + lane, r = x / kPerRow, col = x - r * kPerRow;
-                const uint32_t at = __shfl_sync(kFull, unit, r);
-                const int bytes = valid >> r & 1 ? 16 : 0;
-                if (col < per_row) {
-                    const int64_t off = ((int64_t)at + (bytes ? col : 0)) * 16;
-                    copy16(to + r * S::kRow + col * 16, g.c.k + off, bytes);
-                    copy16(to + S::kHalf + r * S::kRow + col * 16, g.c.v + off, bytes);
+                    for (int x = 0; x < S::kPanels; ++x) {
+                        tiled_load(dst + x * (S::kStep * kPanel), &g.k_map, x * (kPanel / S::kElem), first.in_block, first.entry, &sh.full[to]);
+                        tiled_load(dst + S::kHalf + x * (S::kStep * kPanel), &g.v_map, x * (kPanel / S::kElem), first.in_block, first.entry, &sh.full[to]);
+                    }
+                    if (S::DT == PSMC_F8) {
+                        const int64_t off = (int64_t)first.entry * g.c.blk_bytes + g.c.scale_at + first.in_block;
+                        char* at = pp.ring + to * S::kStage + 2 * S::kHalf + slice * 16;
+                        bulk_load(at, g.c.k + off, 16, &sh.full[to]);
+                        bulk_load(at + S::kScales, g.c.v + off, 16, &sh.full[to]);
+                    }
+                }
+            } else {
+                const uint32_t valid = __ballot_sync(kFull, named);
+                if (kMine >= 16) {
+                    if (lane < kMine / 16) sh.valid[to][warp * (kMine / 16) + lane] = valid >> (lane * 16) & 0xffffu;
+                } else {  // half a slice: a byte of its mask
+                    if (lane == 0) reinterpret_cast<uint16_t*>(&sh.valid[to][warp / 2])[warp % 2] = (uint16_t)valid;
+                }
+                const int64_t off = named ? (int64_t)first.entry * g.c.blk_bytes + (int64_t)first.in_block * (g.c.D * S::kElem) : 0;
+                constexpr int kPerRow = S::kPanels * (kPanel / 16);
+                const int per_row = g.c.D * S::kElem / 16;
+#pragma unroll 4
+                for (int i = 0; i < kMine * kPerRow / 32; ++i) {  // whole rows of panels: what lies beyond the head becomes zero
+                    const int x = i * 32 + lane, r = x / kPerRow, col = x - r * kPerRow, row = warp * kMine + r;
+                    const int64_t from = (int64_t)__shfl_sync(kFull, (long long)off, r) + col * 16;
+                    const int bytes = (valid >> r & 1) && col < per_row ? 16 : 0;
+                    const uint32_t dst = stage + (col / 8) * (S::kStep * kPanel) + row * kPanel + ((col % 8 ^ (row & 7)) << 4);
+                    copy16(dst, g.c.k + (bytes ? from : 0), bytes);
+                    copy16(dst + S::kHalf, g.c.v + (bytes ? from : 0), bytes);
+                }
+                if (S::DT == PSMC_F8) {
+                    scales_at = to;
+                    scales = 127 | 127 << 8;
+                    if (named) {
+                        const int64_t at = (int64_t)first.entry * g.c.blk_bytes + g.c.scale_at + first.in_block;
+                        scales = (int)__ldg(reinterpret_cast<const uint8_t*>(g.c.k) + at) | (int)__ldg(reinterpret_cast<const uint8_t*>(g.c.v) + at) << 8;
+                    }
                 }
             }
-            if (S::DT == PSMC_F8 && lane < kMine) {
-                const int64_t off = named ? (int64_t)first.entry * g.c.blk_bytes + g.c.scale_at + (first.in_block & ~3) : 0;
-                const uint32_t word = stage + 2 * S::kHalf + (warp * kMine + lane) * 4;
-                copy4(word, g.c.k + off, named ? 4 : 0);
-                copy4(word + S::kScales, g.c.v + off, named ? 4 : 0);
-            }
-            if (lane == 0) valid_out[warp] = valid;
         }
-        copies_commit();
+        if (!TILED) copies_commit();
         first = second;
-        second = ask(g, warp, lane);
+        second = ask(g, pp, sh);
+    }
+    // the scale bytes asked for with the step before this one: there by now, and needed a step from now at the earliest
+    __device__ __forceinline__ void put_scales(const Pipe& pp) {
+        if (scales_at >= 0 && pp.lane < kMine) {
+            uint8_t* at = reinterpret_cast<uint8_t*>(pp.ring) + scales_at * S::kStage + 2 * S::kHalf + pp.warp * kMine + pp.lane;
+            at[0] = (uint8_t)scales;
+            at[S::kScales] = (uint8_t)(scales >> 8);
+        }
+        scales_at = -1;
+    }
+    // the next step to be worked on has landed, and everyone is done with the one before it; false: the wait ran out
+    __device__ __forceinline__ bool wait(const Pipe& pp, Shared<S>& sh) {
+        bool ok = true;
+        if (TILED) ok = mbar_wait(&sh.full[pp.stage], pp.phase);
+        else copies_wait<S::kStages - 2>();
+        if (TILED) return __syncthreads_and(ok);
+        __syncthreads();
+        return true;
     }
 };
 
 // row (within the tile) of each place in a segment's mask
 __device__ __forceinline__ void list_rows(uint32_t mask, uint8_t* rows, int lane) {
-    __syncwarp();
     if (mask >> lane & 1) rows[__popc(mask & ((1u << lane) - 1))] = (uint8_t)lane;
     __syncwarp();
 }
 
 template <typename T>
-__device__ __forceinline__ void put(T* p, float x) { *p = from_float<T>(x); }
+__device__ __forceinline__ void put4(T* p, const float4& x) {  // p need not be aligned beyond its type
+    p[0] = from_float<T>(x.x);
+    p[1] = from_float<T>(x.y);
+    p[2] = from_float<T>(x.z);
+    p[3] = from_float<T>(x.w);
+}
 
 // How a CTA's warps divide an item of nq queries: groups of queries, and slices of every step where warps are left over.
 struct Division {
@@ -536,16 +724,68 @@ struct Division {
     }
 };
 
-// ---- the arithmetic of one warp: NT tiles of 8 queries against MT tiles of 16 positions
+__device__ __forceinline__ void next_stage(Pipe& pp, int stages) {
+    if (++pp.stage == stages) {
+        pp.stage = 0;
+        pp.phase ^= 1u;
+    }
+}
+
+// A slice's mask as it is kept: 16 bits, or a byte in each half (copied by position in steps of 32).
+template <class S, bool TILED>
+__device__ __forceinline__ uint32_t slice_valid(const uint32_t* valid, int m) {
+    const uint32_t v = valid[m];
+    return !TILED && S::kStep / kWarps < 16 ? (v & 0xffu) | (v >> 16 & 0xffu) << 8 : v;
+}
+
+// row and query head of query `in_tile` of an item
+template <class S>
+__device__ __forceinline__ void place(const AttendArgs& g, const Item& it, const uint8_t* rows, int in_tile, int* row, int* qh) {
+    const int qi = it.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
+    *row = it.tile * kTileRows + rows[rank];
+    *qh = it.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
+}
+
+// ---- the arithmetic of one warp: NT tiles of 8 queries against tiles of 16 positions
+template <class S>
+struct RawQueries {      // lane (gq, t) holds components of query gq of each tile
+    uint32_t x[2][S::DP / 16][2];
+};
+template <class S>
+__device__ __forceinline__ void load_queries(const AttendArgs& g, const Item& it, const uint8_t* rows, RawQueries<S>& q, const Pipe& pp) {
+    const Division dv(it.nq, S::kGroup, S::kSlices, pp.warp);
+    const int t = pp.lane & 3, gq = pp.lane >> 2, q0 = dv.group * S::kGroup;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        if (j > 0 && it.nq <= 8) break;
+        const int in_tile = q0 + j * 8 + gq;
+        const uint16_t* src = nullptr;
+        if (in_tile < it.nq) {
+            int row, qh;
+            place<S>(g, it, rows, in_tile, &row, &qh);
+            src = static_cast<const uint16_t*>(g.a.q.data) + (int64_t)row * g.a.q.stride_row + (int64_t)qh * g.a.q.stride_head;
+        }
+#pragma unroll
+        for (int ks = 0; ks < S::DP / 16; ++ks)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int d = ks * 16 + (S::DT == PSMC_F8 ? 4 * t + 2 * e : e * 8 + 2 * t);
+                uint32_t x = 0;
+                if (src && d < g.c.D)
+                    x = g.q_words ? __ldg(reinterpret_cast<const uint32_t*>(src + d)) : (uint32_t)__ldg(src + d) | (uint32_t)__ldg(src + d + 1) << 16;
+                q.x[j][ks][e] = x;
+            }
+    }
+}
+
 template <class S, int NT>
 struct Tiles {
     static constexpr bool kF8 = S::DT == PSMC_F8;
     static constexpr int kDt = S::DP / 16;
-    uint32_t q[NT][kDt][2];
     float sc[NT][2];      // queries 2t, 2t + 1 of each tile: factor from product to score in log2 units
     float o[NT][kDt][4], ref[NT][2], sum[NT][2];
 
-    __device__ __forceinline__ void clear() {
+    __device__ __forceinline__ void clear(RawQueries<S>& q, float to_log2, int lane) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             ref[j][0] = ref[j][1] = -INFINITY;
@@ -554,106 +794,106 @@ struct Tiles {
             for (int d = 0; d < kDt; ++d)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[j][d][e] = 0.f;
-        }
-    }
-    // lane (gq, t) holds components of query gq of tile j; src: that query, or NULL
-    __device__ __forceinline__ void load_queries(int j, const uint16_t* src, int D, bool words, float to_log2, int lane) {
-        const int t = lane & 3;
-#pragma unroll
-        for (int ks = 0; ks < kDt; ++ks)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int d = ks * 16 + (kF8 ? 4 * t + 2 * e : e * 8 + 2 * t);
-                uint32_t x = 0;
-                if (src && d < D)
-                    x = words ? __ldg(reinterpret_cast<const uint32_t*>(src + d)) : (uint32_t)__ldg(src + d) | (uint32_t)__ldg(src + d + 1) << 16;
-                q[j][ks][e] = x;
-            }
-        if (!kF8) {
             sc[j][0] = sc[j][1] = to_log2;
-            return;
+            if (!kF8) continue;
+            // fp16 holds a bf16 number's 8 bits but not its range: the query is scaled by a power of two so that its largest
+            // component lies in [128, 256), and the scores get it back
+            float amax = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < kDt; ++ks)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(q.x[j][ks][e] << 16)), fabsf(__uint_as_float(q.x[j][ks][e] & 0xffff0000u))));
+            amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, 2));
+            const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127 - 7, -100), 100);
+            const float inv = pow2i(-ex), back = pow2i(ex) * to_log2;
+#pragma unroll
+            for (int ks = 0; ks < kDt; ++ks)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    q.x[j][ks][e] = pack_f16(__uint_as_float(q.x[j][ks][e] << 16) * inv, __uint_as_float(q.x[j][ks][e] & 0xffff0000u) * inv);
+            sc[j][0] = __shfl_sync(kFull, back, 8 * (lane & 3));
+            sc[j][1] = __shfl_sync(kFull, back, 8 * (lane & 3) + 4);
         }
-        // fp16 holds a bf16 number's 8 bits but not its range: the query is scaled by a power of two so that its largest
-        // component lies in [128, 256), and the scores get it back
-        float amax = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < kDt; ++ks)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(q[j][ks][e] << 16)), fabsf(__uint_as_float(q[j][ks][e] & 0xffff0000u))));
-        amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(kFull, amax, 2));
-        const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127 - 7, -100), 100);
-        const float inv = pow2i(-ex), back = pow2i(ex) * to_log2;
-#pragma unroll
-        for (int ks = 0; ks < kDt; ++ks)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                q[j][ks][e] = pack_f16(__uint_as_float(q[j][ks][e] << 16) * inv, __uint_as_float(q[j][ks][e] & 0xffff0000u) * inv);
-        sc[j][0] = __shfl_sync(kFull, back, 8 * t);
-        sc[j][1] = __shfl_sync(kFull, back, 8 * t + 4);
     }
 
-    // keys, vals: shared addresses of 16 rows; valid: which of them hold something; k_scale, v_byte: lane p's scales (8-bit)
-    __device__ __forceinline__ void step(uint32_t keys, uint32_t vals, uint32_t valid, float k_scale, int v_byte, int lane) {
+    // MT slices: keys[m], vals[m]: shared addresses of their 16 rows; valid[m]: which of them hold something; k_scale[m],
+    // v_byte[m]: lane p's scales (8-bit)
+    template <int MT>
+    __device__ __forceinline__ void step(const RawQueries<S>& q, const uint32_t (&keys)[MT], const uint32_t (&vals)[MT], const uint32_t (&valid)[MT],
+                                         const float (&k_scale)[MT], const int (&v_byte)[MT], int lane) {
         const int gq = lane >> 2;
-        float s[NT][4], s2[NT][4];  // two chains, so that the products of one tile wait less for each other
+        float s[MT][NT][4], s2[MT][NT][4];  // two chains, so that the products of one tile wait less for each other
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[j][e] = s2[j][e] = 0.f;
-        const uint32_t krow = keys + (lane & 15) * S::kRow + (lane >> 4) * 16;
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[m][j][e] = s2[m][j][e] = 0.f;
+        // unit u of a row lies at u ^ (row % 8); the lane's row, and its unit before the exchange within a pair
+        const uint32_t krow = (lane & 15) * kPanel, kunit = ((lane >> 4) ^ (lane & 7)) << 4;
         if (!kF8) {
 #pragma unroll
-            for (int ks = 0; ks < kDt; ++ks) {
-                uint32_t ka[4];
-                load_tiles(ka, krow + ks * 32);
+            for (int ks = 0; ks < kDt; ++ks)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) mma<false>(ks & 1 ? s2[j] : s[j], ka, q[j][ks][0], q[j][ks][1]);
-            }
+                for (int m = 0; m < MT; ++m) {
+                    uint32_t ka[4];
+                    load_tiles(ka, keys[m] + krow + (2 * ks / 8) * (S::kStep * kPanel) + ((2 * ks % 8 << 4) ^ kunit));
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) mma<false>(ks & 1 ? s2[m][j] : s[m][j], ka, q.x[j][ks][0], q.x[j][ks][1]);
+                }
         } else {
 #pragma unroll
-            for (int ks = 0; ks < kDt; ks += 2) {  // 32 components: two tiles of 16
-                uint32_t kc[4];
-                load_tiles(kc, krow + ks * 16);
+            for (int ks = 0; ks < kDt; ks += 2)  // 32 components: two tiles of 16
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t ka[4] = {codes_to_f16(kc[2 * u]), codes_to_f16(kc[2 * u + 1]), codes_to_f16(kc[2 * u] >> 16),
-                                            codes_to_f16(kc[2 * u + 1] >> 16)};
+                for (int m = 0; m < MT; ++m) {
+                    uint32_t kc[4];
+                    load_tiles(kc, keys[m] + krow + (ks / 8) * (S::kStep * kPanel) + ((ks % 8 << 4) ^ kunit));
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) mma<true>(u ? s2[j] : s[j], ka, q[j][ks + u][0], q[j][ks + u][1]);
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t ka[4] = {codes_to_f16(kc[2 * u]), codes_to_f16(kc[2 * u + 1]), codes_to_f16(kc[2 * u] >> 16),
+                                                codes_to_f16(kc[2 * u + 1] >> 16)};
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) mma<true>(u ? s2[m][j] : s[m][j], ka, q.x[j][ks + u][0], q.x[j][ks + u][1]);
+                    }
                 }
-            }
         }
         // scaled to log2 units; positions without anything get -inf
-        float ev0 = 0.f, ev1 = 0.f, iv0 = 1.f, iv1 = 1.f, ks0 = 1.f, ks1 = 1.f;  // 8-bit: scales of positions gq, gq + 8
-        if (kF8) {
-            ks0 = __shfl_sync(kFull, k_scale, gq);
-            ks1 = __shfl_sync(kFull, k_scale, gq + 8);
-            const int b0 = __shfl_sync(kFull, v_byte, gq), b1 = __shfl_sync(kFull, v_byte, gq + 8);
-            ev0 = (float)(b0 - 127);
-            ev1 = (float)(b1 - 127);
-            iv0 = __uint_as_float((uint32_t)(254 - b0) << 23);
-            iv1 = __uint_as_float((uint32_t)(254 - b1) << 23);
-        }
-        const bool ok0 = valid >> gq & 1, ok1 = valid >> (gq + 8) & 1;
+        float iv[MT][2];
         bool grow = false;
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = (s[j][e] + s2[j][e]) * sc[j][e & 1];
-                if (kF8) x = fmaf(x, e < 2 ? ks0 : ks1, e < 2 ? ev0 : ev1);
-                x = (e < 2 ? ok0 : ok1) ? x : -INFINITY;
-                s[j][e] = x;
-                grow = grow || x > ref[j][e & 1] + kSlack;
+        for (int m = 0; m < MT; ++m) {
+            const bool ok0 = valid[m] >> gq & 1, ok1 = valid[m] >> (gq + 8) & 1;
+            float ev0 = 0.f, ev1 = 0.f, ks0 = 1.f, ks1 = 1.f;  // 8-bit: scales of positions gq, gq + 8
+            if (kF8) {
+                ks0 = __shfl_sync(kFull, k_scale[m], gq);
+                ks1 = __shfl_sync(kFull, k_scale[m], gq + 8);
+                const int b0 = __shfl_sync(kFull, v_byte[m], gq), b1 = __shfl_sync(kFull, v_byte[m], gq + 8);
+                ev0 = (float)(b0 - 127);
+                ev1 = (float)(b1 - 127);
+                iv[m][0] = ok0 ? __uint_as_float((uint32_t)(254 - b0) << 23) : 0.f;
+                iv[m][1] = ok1 ? __uint_as_float((uint32_t)(254 - b1) << 23) : 0.f;
             }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = (s[m][j][e] + s2[m][j][e]) * sc[j][e & 1];
+                    if (kF8) x = fmaf(x, e < 2 ? ks0 : ks1, e < 2 ? ev0 : ev1);
+                    x = (e < 2 ? ok0 : ok1) ? x : -INFINITY;
+                    s[m][j][e] = x;
+                    grow = grow || x > ref[j][e & 1] + kSlack;
+                }
+        }
         if (__any_sync(kFull, grow)) {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float top = fmaxf(ref[j][i], fmaxf(s[j][i], s[j][i + 2]));
+                    float top = ref[j][i];
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) top = fmaxf(top, fmaxf(s[m][j][i], s[m][j][i + 2]));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
@@ -668,58 +908,64 @@ struct Tiles {
                 }
         }
         // weights, as the second operand of O^T += V^T P^T: [positions, queries], turned 8 x 8 at a time
-        uint32_t p[NT][kF8 ? 1 : 2][2];
+        uint32_t p[MT][NT][kF8 ? 1 : 2][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const float r0 = ref[j][0] == -INFINITY ? 0.f : ref[j][0], r1 = ref[j][1] == -INFINITY ? 0.f : ref[j][1];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float p0 = ex2(s[j][2 * h] - r0), p1 = ex2(s[j][2 * h + 1] - r1);
-                if (kF8) {
-                    // weights of the codes: the values' scale is in the exponent already, and the sum takes it out again.
-                    // fp16 holds 11 bits of a weight down to 2^-14 of the largest
-                    sum[j][0] = fmaf(p0, h ? iv1 : iv0, sum[j][0]);
-                    sum[j][1] = fmaf(p1, h ? iv1 : iv0, sum[j][1]);
-                    p[j][0][h] = turn_tile(pack_f16(p0, p1));
-                } else {
-                    // a weight as the sum of two bf16 numbers: 16 bits of it instead of 8
-                    sum[j][0] += p0;
-                    sum[j][1] += p1;
-                    const uint32_t hi = pack_bf16(p0, p1);
-                    p[j][0][h] = turn_tile(hi);
-                    p[j][kF8 ? 0 : 1][h] = turn_tile(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float p0 = ex2(s[m][j][2 * h] - r0), p1 = ex2(s[m][j][2 * h + 1] - r1);
+                    if (kF8) {
+                        // weights of the codes: the values' scale is in the exponent already, and the sum takes it out again;
+                        // fp16 holds 11 bits of a weight down to 2^-14 of the largest
+                        sum[j][0] = fmaf(p0, iv[m][h], sum[j][0]);
+                        sum[j][1] = fmaf(p1, iv[m][h], sum[j][1]);
+                        p[m][j][0][h] = turn_tile(pack_f16(p0, p1));
+                    } else {
+                        // a weight as the sum of two bf16 numbers: 16 bits of it instead of 8
+                        sum[j][0] += p0;
+                        sum[j][1] += p1;
+                        const uint32_t hi = pack_bf16(p0, p1);
+                        p[m][j][0][h] = turn_tile(hi);
+                        p[m][j][kF8 ? 0 : 1][h] = turn_tile(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+                    }
                 }
-            }
         }
-        const uint32_t vrow = vals + ((lane & 7) + (lane >> 4) * 8) * S::kRow + (lane >> 3 & 1) * 16;
+        const uint32_t vrow = ((lane & 7) + (lane >> 4) * 8) * kPanel, vunit = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
         if (!kF8) {
 #pragma unroll
-            for (int d = 0; d < kDt; ++d) {
-                uint32_t va[4];
-                load_tiles_turned(va, vrow + d * 32);
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    mma<false>(o[j][d], va, p[j][0][0], p[j][0][1]);
-                    mma<false>(o[j][d], va, p[j][kF8 ? 0 : 1][0], p[j][kF8 ? 0 : 1][1]);
+                for (int d = 0; d < kDt; ++d) {
+                    uint32_t va[4];
+                    load_tiles_turned(va, vals[m] + vrow + (2 * d / 8) * (S::kStep * kPanel) + ((2 * d % 8 << 4) ^ vunit));
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        mma<false>(o[j][d], va, p[m][j][0][0], p[m][j][0][1]);
+                        mma<false>(o[j][d], va, p[m][j][kF8 ? 0 : 1][0], p[m][j][kF8 ? 0 : 1][1]);
+                    }
                 }
-            }
         } else {
 #pragma unroll
-            for (int d = 0; d < kDt; d += 2) {  // 32 components: the even ones, then the odd ones
-                uint32_t vc[4], va[2][4];
-                load_tiles_turned(vc, vrow + d * 16);
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {  // bytes (pos 0, d), (pos 0, d + 1), (pos 1, d), (pos 1, d + 1)
-                    const uint32_t x = __byte_perm(vc[e], 0, 0x3120);
-                    va[0][e] = codes_to_f16(x);
-                    va[1][e] = codes_to_f16(x >> 16);
-                }
+                for (int d = 0; d < kDt; d += 2) {  // 32 components: the even ones, then the odd ones
+                    uint32_t vc[4], va[2][4];
+                    load_tiles_turned(vc, vals[m] + vrow + (d / 8) * (S::kStep * kPanel) + ((d % 8 << 4) ^ vunit));
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    mma<true>(o[j][d], va[0], p[j][0][0], p[j][0][1]);
-                    mma<true>(o[j][d + 1], va[1], p[j][0][0], p[j][0][1]);
+                    for (int e = 0; e < 4; ++e) {  // bytes (pos 0, d), (pos 0, d + 1), (pos 1, d), (pos 1, d + 1)
+                        const uint32_t x = __byte_perm(vc[e], 0, 0x3120);
+                        va[0][e] = codes_to_f16(x);
+                        va[1][e] = codes_to_f16(x >> 16);
+                    }
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        mma<true>(o[j][d], va[0], p[m][j][0][0], p[m][j][0][1]);
+                        mma<true>(o[j][d + 1], va[1], p[m][j][0][0], p[m][j][0][1]);
+                    }
                 }
-            }
         }
     }
     // component of the output that o[j][d][2 * e + i] of a lane belongs to (query 2t + i): see the tiles above
@@ -728,83 +974,124 @@ struct Tiles {
     }
 };
 
-struct Pipe {            // the ring of stages as a CTA sees it
-    char* ring;
-    uint32_t ring_at;
-    uint32_t (*valid)[kWarps];
-    int stage;           // the stage of the next step to be consumed
-};
-
-// Columns beyond the head are zero in every stage (a product with what lies there must not be NaN); a stage that carried
-// outputs is put right again.
+// Values of positions that hold nothing become zero (their weights are, but what lies there may be NaN): rows of the one
+// slice at a segment's end that a tiled copy brought along.
 template <class S>
-__device__ __forceinline__ void clear_margin(const Pipe& pipe, int stage, int D) {
-    if (D >= S::DP) return;
-    __syncthreads();
-    constexpr int kUnits = S::DP * S::kElem / 16;
-    const int first = D * S::kElem / 16, per_row = kUnits - first;
-    for (int x = threadIdx.x; x < 2 * S::kStep * per_row; x += kWarps * 32) {
-        const int r = x / per_row, col = first + x - r * per_row;
-        *reinterpret_cast<uint4*>(pipe.ring + stage * S::kStage + r * S::kRow + col * 16) = uint4{0, 0, 0, 0};
+__device__ __forceinline__ void clear_rows(char* vals, uint32_t valid, int lane) {
+    for (uint32_t dead = ~valid & 0xffffu; dead; dead &= dead - 1) {
+        const int r = __ffs(dead) - 1;
+        for (int u = lane; u < S::kPanels * 8; u += 32)
+            *reinterpret_cast<uint4*>(vals + (u / 8) * (S::kStep * kPanel) + r * kPanel + (u % 8) * 16) = uint4{0, 0, 0, 0};
+    }
+    fence_async_smem();  // before a copy may write there again
+    __syncwarp();
+}
+
+// One tile of 8 queries of every warp, outputs in `carry` [warp][query][DP + 4] as shares of the largest reference of their
+// slices: summed over the slices and written, to the queries' rows or as partial results, 16 bytes per lane.  first: the
+// tile's first query within a warp's group.
+template <class S>
+__device__ __forceinline__ void write_tile(const AttendArgs& g, const Item& it, const Division& dv, const float* carry, const Shared<S>& sh,
+                                           const uint8_t* rows, int first, const Pipe& pp) {
+    using T = typename PoolIo<S::DT>::type;
+    constexpr int kPitch = S::DP + 4;
+    for (int u = 0; u < 2 * dv.groups; ++u) {  // the warps share the queries evenly
+        const int x = pp.warp * 2 * dv.groups + u, grp = x >> 3, ql = x & 7, in_tile = grp * S::kGroup + first + ql;
+        if (in_tile >= it.nq || first + ql >= S::kGroup) continue;
+        float top = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int z = 0; z < kWarps; ++z)
+            if (z < dv.slices) {
+                top = fmaxf(top, sh.stats[z * dv.groups + grp][first + ql].x);
+                total += sh.scaled[z * dv.groups + grp][first + ql];
+            }
+        int row, qh;
+        place<S>(g, it, rows, in_tile, &row, &qh);
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int i = 0; i < (S::DP + 127) / 128; ++i) {
+            const int d = pp.lane * 4 + i * 128;
+            if (d >= g.c.D) continue;
+            float4 o = float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int z = 0; z < kWarps; ++z)
+                if (z < dv.slices) {
+                    const float4 y = *reinterpret_cast<const float4*>(carry + ((z * dv.groups + grp) * 8 + ql) * kPitch + d);
+                    o.x += y.x;
+                    o.y += y.y;
+                    o.z += y.z;
+                    o.w += y.w;
+                }
+            if (it.alone) {
+                o = float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+                put4(static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head + d, o);
+            } else {
+                *reinterpret_cast<float4*>(g.l.part + (it.slot + in_tile) * g.c.D + d) = o;
+            }
+        }
+        if (pp.lane == 0) {
+            if (!it.alone) g.l.stat[it.slot + in_tile] = float2{top, total};
+            else if (g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total == 0.f ? -INFINITY : kLn2 * (top + log2f(total));
+        }
     }
 }
 
-// One item, from its queries to its result.  NT: tiles of 8 queries per warp.
-template <class S, int NT>
-__device__ __forceinline__ void run_item(const AttendArgs& g, Walk& cur, Feeder<S>& feed, Pipe& pipe, uint8_t* row_list, float2 (*stats)[16],
-                                         int worker, int lane, int warp) {
-    using T = typename PoolIo<S::DT>::type;
+// One item, from its queries (already asked for) to its result.  NT: tiles of 8 queries per warp.
+template <class S, bool TILED, int NT>
+__device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, RawQueries<S>& q, Feeder<S, TILED>& feed, Pipe& pp, Shared<S>& sh,
+                                         int index) {
     using Ti = Tiles<S, NT>;
     constexpr bool kF8 = S::DT == PSMC_F8;
-    const Division dv(cur.nq, S::kGroup, S::kSlices, warp);
-    const int t = lane & 3, gq = lane >> 2;
-    list_rows(cur.mask, row_list, lane);
-    const int q0 = dv.group * S::kGroup, mine = dv.slice < dv.slices ? min(S::kGroup, cur.nq - q0) : 0;  // may be <= 0
-    const auto place = [&](int in_tile, int* row, int* qh) {
-        const int qi = cur.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
-        *row = cur.tile * kTileRows + row_list[rank];
-        *qh = cur.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
-    };
+    constexpr int kMost = NT == 1 || S::DP <= 128 ? S::kPair : 1;  // slices at a time
+    const int lane = pp.lane, warp = pp.warp, t = lane & 3, gq = lane >> 2;
+    const Division dv(it.nq, S::kGroup, S::kSlices, warp);
+    const bool busy = dv.slice < dv.slices && dv.group * S::kGroup < it.nq;
     Ti ti;
-    ti.clear();
+    ti.clear(q, g.a.scale * kLog2e, lane);
+#pragma unroll 1
+    for (int s = 0; s < it.steps; ++s) {
+        if (!feed.wait(pp, sh)) return false;
+        feed.issue(g, pp.stage == 0 ? S::kStages - 1 : pp.stage - 1, pp, sh);
+        if (busy) {
+            char* at = pp.ring + pp.stage * S::kStage;
+#pragma unroll 1
+            for (int m0 = dv.slice; m0 < S::kSlices; m0 += kMost * dv.slices) {
+                uint32_t keys[kMost], vals[kMost], valid[kMost];
+                float k_scale[kMost];
+                int v_byte[kMost];
+                uint32_t any = 0;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const uint16_t* src = nullptr;
-        if (j * 8 + gq < mine) {
-            int row, qh;
-            place(q0 + j * 8 + gq, &row, &qh);
-            src = static_cast<const uint16_t*>(g.a.q.data) + (int64_t)row * g.a.q.stride_row + (int64_t)qh * g.a.q.stride_head;
-        }
-        ti.load_queries(j, src, g.c.D, g.q_words, g.a.scale * kLog2e, lane);
-    }
-    int stage = pipe.stage;
-#pragma unroll 1
-    for (; cur.s < cur.s_end; ++cur.s) {
-        copies_wait<S::kStages - 2>();
-        __syncthreads();  // this step has landed for everyone, and everyone is done with the one before it
-        const int ahead = stage == 0 ? S::kStages - 1 : stage - 1;
-        feed.issue(g, pipe.ring_at + ahead * S::kStage, pipe.valid[ahead], warp, lane);
-        if (mine > 0) {
-            const uint32_t keys = pipe.ring_at + stage * S::kStage;
-#pragma unroll 1
-            for (int m = dv.slice; m < S::kSlices; m += dv.slices) {
-                const uint32_t valid = pipe.valid[stage][m * kWarps / S::kSlices];
-                if (valid == 0) continue;  // beyond the segment
-                float k_scale = 1.f;
-                int v_byte = 127;
-                if (kF8) {  // lane p's scale bytes
-                    const int p = cur.p0 + cur.s * S::kStep + m * 16 + (lane & 15);
-                    const int off = p - div_by(p, g.by_block) * g.c.block_len, shift = ((cur.head * g.c.block_len + off) & 3) * 8;
-                    const uint32_t* words = reinterpret_cast<const uint32_t*>(pipe.ring + stage * S::kStage + 2 * S::kHalf) + m * 16 + (lane & 15);
-                    k_scale = __uint_as_float((words[0] >> shift & 255u) << 23);
-                    v_byte = (int)(words[S::kStep] >> shift & 255u);
+                for (int i = 0; i < kMost; ++i) {
+                    const int m = m0 + i * dv.slices;
+                    keys[i] = smem_of(at) + m * 16 * kPanel;
+                    vals[i] = keys[i] + S::kHalf;
+                    valid[i] = slice_valid<S, TILED>(sh.valid[pp.stage], m);
+                    any |= valid[i];
+                    k_scale[i] = 1.f;
+                    v_byte[i] = 127;
+                    if (kF8) {  // lane p's scale bytes
+                        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(at) + 2 * S::kHalf + m * 16 + (lane & 15);
+                        k_scale[i] = __uint_as_float((uint32_t)bytes[0] << 23);
+                        v_byte[i] = bytes[S::kScales];
+                    }
                 }
-                ti.step(keys + m * 16 * S::kRow, keys + S::kHalf + m * 16 * S::kRow, valid, k_scale, v_byte, lane);
+                if (any == 0) continue;  // beyond the segment
+                if (TILED)
+#pragma unroll
+                    for (int i = 0; i < kMost; ++i)
+                        if (valid[i] != 0xffffu) clear_rows<S>(at + S::kHalf + (m0 + i * dv.slices) * 16 * kPanel, valid[i], lane);
+                ti.template step<kMost>(q, keys, vals, valid, k_scale, v_byte, lane);
             }
         }
-        stage = stage + 1 == S::kStages ? 0 : stage + 1;
+        next_stage(pp, S::kStages);
     }
-    pipe.stage = stage;
+    // ---- the next item's queries travel while this one's result is put together
+    if (index + 1 < feed.items) {
+        const Item next = sh.queue[(index + 1) % kQueue];
+        uint8_t* rows = sh.rows[(index + 1) & 1][warp];
+        list_rows(next.mask, rows, lane);
+        load_queries<S>(g, next, rows, q, pp);
+    }
     // ---- sums over the lanes that hold parts of them, then over the slices
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -815,312 +1102,263 @@ __device__ __forceinline__ void run_item(const AttendArgs& g, Walk& cur, Feeder<
             x += __shfl_xor_sync(kFull, x, 8);
             x += __shfl_xor_sync(kFull, x, 16);
             ti.sum[j][i] = x;
+            if (gq == 0) sh.stats[warp][j * 8 + 2 * t + i] = float2{ti.ref[j][i], x};
         }
-    if (dv.slices > 1) {
-        if (gq == 0)
+    __syncthreads();  // also: everyone is done with the last step's stage, which now carries the outputs
+    float* carry = reinterpret_cast<float*>(pp.ring + (pp.stage == 0 ? S::kStages - 1 : pp.stage - 1) * S::kStage);
+    constexpr int kPitch = S::DP + 4;
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) stats[warp][j * 8 + 2 * t + i] = float2{ti.ref[j][i], ti.sum[j][i]};
-        __syncthreads();  // also: everyone is done with the last step's stage, which now carries the outputs
-        const int used = stage == 0 ? S::kStages - 1 : stage - 1;
-        float* carry = reinterpret_cast<float*>(pipe.ring + used * S::kStage);  // [slice - 1 or group][component][8 queries]
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
+    for (int j = 0; j < NT; ++j) {
+        if (busy)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float top = -INFINITY, all = 0.f;
-                for (int z = 0; z < dv.slices; ++z) top = fmaxf(top, stats[z * dv.groups + dv.group][j * 8 + 2 * t + i].x);
-                for (int z = 0; z < dv.slices; ++z) {
-                    const float2 st = stats[z * dv.groups + dv.group][j * 8 + 2 * t + i];
-                    all += st.x == -INFINITY ? 0.f * st.y : st.y * (st.x == top ? 1.f : ex2(st.x - top));
-                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int z = 0; z < kWarps; ++z)
+                    if (z < dv.slices) top = fmaxf(top, sh.stats[z * dv.groups + dv.group][j * 8 + 2 * t + i].x);
+                // (a factor of zero keeps a NaN that came with the values)
                 const float f = ti.ref[j][i] == top ? 1.f : (ti.ref[j][i] == -INFINITY ? 0.f : ex2(ti.ref[j][i] - top));
-                ti.ref[j][i] = top;
-                ti.sum[j][i] = all;
-#pragma unroll
-                for (int d = 0; d < Ti::kDt; ++d) {
-                    ti.o[j][d][i] *= f;
-                    ti.o[j][d][i + 2] *= f;
-                }
-            }
-            float* at = carry + ((dv.slice - 1) * dv.groups + dv.group) * (8 * S::DP);
-            if (dv.slice > 0 && mine > 0) {
+                if (gq == 0) sh.scaled[warp][j * 8 + 2 * t + i] = ti.sum[j][i] * f;
 #pragma unroll
                 for (int d = 0; d < Ti::kDt; ++d)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) at[(d * 4 + e) * 32 + lane] = ti.o[j][d][e];
+                    for (int e = 0; e < 2; ++e)
+                        carry[(warp * 8 + 2 * t + i) * kPitch + Ti::component(d, e, lane)] = ti.o[j][d][2 * e + i] * f;
             }
-            __syncthreads();
-            if (dv.slice == 0 && mine > 0)
-                for (int z = 1; z < dv.slices; ++z) {
-                    const float* from = carry + ((z - 1) * dv.groups + dv.group) * (8 * S::DP);
-#pragma unroll
-                    for (int d = 0; d < Ti::kDt; ++d)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) ti.o[j][d][e] += from[(d * 4 + e) * 32 + lane];
-                }
-            if (j + 1 < NT) __syncthreads();
-        }
-        clear_margin<S>(pipe, used, g.c.D);
-    }
-    if (dv.slice != 0) return;
-    const bool alone = cur.alone(g.l);
-    const int64_t slot = cur.slot(g.l, worker);
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int in_group = j * 8 + 2 * t + i;
-            if (in_group >= mine) continue;
-            const float total = ti.sum[j][i];
-            if (!alone) {
-                float* part = g.l.part + (slot + q0 + in_group) * g.c.D;
-#pragma unroll
-                for (int d = 0; d < Ti::kDt; ++d)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int at = Ti::component(d, e, lane);
-                        if (at < g.c.D) part[at] = ti.o[j][d][2 * e + i];
-                    }
-                if (gq == 0) g.l.stat[slot + q0 + in_group] = float2{ti.ref[j][i], total};
-                continue;
-            }
-            int row, qh;
-            place(q0 + in_group, &row, &qh);
-            T* out = static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head;
-            const float inv = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-            for (int d = 0; d < Ti::kDt; ++d)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int at = Ti::component(d, e, lane);
-                    if (at < g.c.D) put(out + at, ti.o[j][d][2 * e + i] * inv);
-                }
-            if (gq == 0 && g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total == 0.f ? -INFINITY : kLn2 * (ti.ref[j][i] + log2f(total));
-        }
-}
-
-template <class S>
-__device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, uint32_t (*valid)[kWarps], Pipe* pipe, Feeder<S>* feed, Walk* cur,
-                                          int worker, int warp, int lane) {
-    pipe->ring = smem;
-    pipe->ring_at = smem_of(smem);
-    pipe->valid = valid;
-    pipe->stage = 0;
-    if (g.c.D < S::DP) {  // columns beyond the head: never copied, always zero
-        for (int i = threadIdx.x; i < S::kStages * S::kStage / 16; i += kWarps * 32) reinterpret_cast<uint4*>(smem)[i] = uint4{0, 0, 0, 0};
         __syncthreads();
+        write_tile<S>(g, it, dv, carry, sh, sh.rows[index & 1][warp], j * 8, pp);
+        if (j + 1 < NT) __syncthreads();
     }
-    chain_begin();
-    feed->walk.begin(g.l, worker, lane);
-    *cur = feed->walk;
-    if (cur->done) return false;
-    feed->begin(g, warp, lane);
-#pragma unroll 1
-    for (int i = 0; i < S::kStages - 1; ++i) feed->issue(g, pipe->ring_at + i * S::kStage, valid[i], warp, lane);
+    if (TILED) fence_async_smem();  // before a copy may write there again
     return true;
 }
 
+template <class S, bool TILED>
+__device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe& pp, Shared<S>& sh, Feeder<S, TILED>& feed) {
+    pp.ring = smem + (-(int)smem_of(smem) & 1023);
+    pp.ring_at = smem_of(pp.ring);
+    pp.stage = 0;
+    pp.phase = 0;
+    pp.lane = threadIdx.x & 31;
+    pp.warp = threadIdx.x >> 5;
+    pp.worker = blockIdx.x;
+    if (TILED && threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) mbar_init(&sh.full[i], kWarps);
+        fence_async_smem();
+    }
+    chain_begin();
+    feed.walk.begin(g.l, pp.worker, pp.lane);
+    feed.items = feed.asked = 0;
+    feed.scales_at = -1;
+    if (feed.walk.done) return false;
+    feed.first = feed.ask(g, pp, sh);
+    feed.second = feed.ask(g, pp, sh);
+    __syncthreads();  // the barriers are ready, the first item is in the queue
+    return true;
+}
+template <class S, bool TILED>
+__device__ __forceinline__ void fill_pipe(const AttendArgs& g, Pipe& pp, Shared<S>& sh, Feeder<S, TILED>& feed) {
+#pragma unroll 1
+    for (int i = 0; i < S::kStages - 1; ++i) feed.issue(g, i, pp, sh);
+}
+// A wait for a copy ran out: says so, and gives the copies that are still on their way their time before the CTA ends.
 template <class S>
-__global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_kernel(const AttendArgs g) {
-    extern __shared__ __align__(16) char smem[];
-    __shared__ uint32_t valid[S::kStages][kWarps];
-    __shared__ uint8_t row_list[kWarps][kTileRows];
-    __shared__ float2 stats[kWarps][16];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = blockIdx.x;
-    Pipe pipe;
-    Feeder<S> feed;
-    Walk cur;
-    if (!open_pipe<S>(g, smem, valid, &pipe, &feed, &cur, worker, warp, lane)) return;
-    while (!cur.done) {
-        if (cur.nq <= 8) run_item<S, 1>(g, cur, feed, pipe, row_list[warp], stats, worker, lane, warp);
-        else run_item<S, 2>(g, cur, feed, pipe, row_list[warp], stats, worker, lane, warp);
-        cur.next_item(g.l);
+__device__ __forceinline__ void give_up(const AttendArgs& g, const Pipe& pp, Shared<S>& sh) {
+    if (threadIdx.x == 0) raise_status(g.a.status, PSMC_E_TIMEOUT);
+    int stage = pp.stage;
+    uint32_t phase = pp.phase;
+    for (int i = 0; i < S::kStages; ++i) {
+        mbar_wait(&sh.full[stage], phase);
+        if (++stage == S::kStages) {
+            stage = 0;
+            phase ^= 1u;
+        }
     }
 }
 
-// 32-bit caches: no matrix unit holds 24 bits, so the products are plain multiplications.  A slice's 16 x 8 scores are four
-// per lane (one position, four queries); in the second product a lane owns DP / 32 components of all 8 queries.
-template <class S>
-__global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_f32_kernel(const AttendArgs g) {
+template <class S, bool TILED>
+__global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_kernel(const __grid_constant__ AttendArgs g) {
+    extern __shared__ __align__(1024) char smem[];
+    __shared__ Shared<S> sh;
+    static_assert(sizeof(sh) <= S::kBeside, "beside the ring");
+    Pipe pp;
+    Feeder<S, TILED> feed;
+    if (!open_pipe<S, TILED>(g, smem, pp, sh, feed)) return;
+    RawQueries<S> q;
+    {
+        const Item it = sh.queue[0];
+        list_rows(it.mask, sh.rows[0][pp.warp], pp.lane);
+        load_queries<S>(g, it, sh.rows[0][pp.warp], q, pp);
+    }
+    fill_pipe<S, TILED>(g, pp, sh, feed);
+    for (int index = 0; index < feed.items; ++index) {
+        const Item it = sh.queue[index % kQueue];
+        const bool ok = it.nq <= 8 ? run_item<S, TILED, 1>(g, it, q, feed, pp, sh, index) : run_item<S, TILED, 2>(g, it, q, feed, pp, sh, index);
+        if (!ok) {
+            give_up<S>(g, pp, sh);
+            return;
+        }
+    }
+}
+
+// 32-bit caches: no matrix unit holds 24 bits, so the products are plain multiplications.  NQ queries per warp.  A slice's
+// scores: a lane has one position, and four queries (NQ = 8) or half of the components of four (NQ = 4); in the second
+// product a lane owns DP / 32 components of all queries.
+template <class S, bool TILED, int NQ>
+__device__ __forceinline__ bool run_item_f32(const AttendArgs& g, const Item& it, float* qs, float* ps, Feeder<S, TILED>& feed, Pipe& pp,
+                                             Shared<S>& sh, int index) {
     constexpr int kOwn = S::DP / 32;
-    extern __shared__ __align__(16) char smem[];
-    __shared__ uint32_t valid[S::kStages][kWarps];
-    __shared__ uint8_t row_list[kWarps][kTileRows];
-    __shared__ float2 stats[kWarps][8];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = blockIdx.x, key = lane & 15, qh4 = (lane >> 4) * 4;
-    float* qs = reinterpret_cast<float*>(smem + S::kStages * S::kStage) + warp * (8 * S::DP + 16 * 8);  // [8][DP]
-    float* ps = qs + 8 * S::DP;                                                                         // [16][8]
-    Pipe pipe;
-    Feeder<S> feed;
-    Walk cur;
-    if (!open_pipe<S>(g, smem, valid, &pipe, &feed, &cur, worker, warp, lane)) return;
+    static_assert(S::kPair == 1, "one slice at a time");
+    const int lane = pp.lane, warp = pp.warp, key = lane & 15, half = lane >> 4, qh4 = NQ == 8 ? half * 4 : 0;
+    const Division dv(it.nq, S::kGroup, S::kSlices, warp);
+    const int q0 = dv.group * S::kGroup, mine = dv.slice < dv.slices ? min(S::kGroup, it.nq - q0) : 0;  // may be <= 0
+    const uint8_t* rows = sh.rows[index & 1][warp];
+    {
+        float x[NQ][kOwn];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            int row = 0, qh = 0;
+            if (j < mine) place<S>(g, it, rows, q0 + j, &row, &qh);
+            const float* q = static_cast<const float*>(g.a.q.data) + (int64_t)row * g.a.q.stride_row + (int64_t)qh * g.a.q.stride_head;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) x[j][i] = j < mine && lane + 32 * i < g.c.D ? __ldg(q + lane + 32 * i) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < NQ; ++j)
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) qs[j * S::DP + lane + 32 * i] = x[j][i];
+    }
     const float to_log2 = g.a.scale * kLog2e;
-    while (!cur.done) {
-        const Division dv(cur.nq, S::kGroup, S::kSlices, warp);
-        list_rows(cur.mask, row_list[warp], lane);
-        const int q0 = dv.group * S::kGroup, mine = dv.slice < dv.slices ? min(S::kGroup, cur.nq - q0) : 0;  // may be <= 0
-        const auto place = [&](int in_tile, int* row, int* qh) {
-            const int qi = cur.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
-            *row = cur.tile * kTileRows + row_list[warp][rank];
-            *qh = cur.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
-        };
-        {
-            float x[8][kOwn];
+    float o[NQ][kOwn], ref[4], sum[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                int row = 0, qh = 0;
-                if (j < mine) place(q0 + j, &row, &qh);
-                const float* q = static_cast<const float*>(g.a.q.data) + (int64_t)row * g.a.q.stride_row + (int64_t)qh * g.a.q.stride_head;
+    for (int j = 0; j < NQ; ++j)
 #pragma unroll
-                for (int i = 0; i < kOwn; ++i) x[j][i] = j < mine && lane + 32 * i < g.c.D ? __ldg(q + lane + 32 * i) : 0.f;
-            }
+        for (int i = 0; i < kOwn; ++i) o[j][i] = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int i = 0; i < kOwn; ++i) qs[j * S::DP + lane + 32 * i] = x[j][i];
-        }
-        float o[8][kOwn], ref[4], sum[4];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) o[j][i] = 0.f;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            ref[u] = -INFINITY;
-            sum[u] = 0.f;
-        }
-        __syncwarp();
-        int stage = pipe.stage;
+    for (int u = 0; u < 4; ++u) {
+        ref[u] = -INFINITY;
+        sum[u] = 0.f;
+    }
+    __syncwarp();
 #pragma unroll 1
-        for (; cur.s < cur.s_end; ++cur.s) {
-            copies_wait<S::kStages - 2>();
-            __syncthreads();  // this step has landed for everyone, and everyone is done with the one before it
-            const int ahead = stage == 0 ? S::kStages - 1 : stage - 1;
-            feed.issue(g, pipe.ring_at + ahead * S::kStage, pipe.valid[ahead], warp, lane);
+    for (int st = 0; st < it.steps; ++st) {
+        if (!feed.wait(pp, sh)) return false;
+        feed.issue(g, pp.stage == 0 ? S::kStages - 1 : pp.stage - 1, pp, sh);
 #pragma unroll 1
-            for (int m = dv.slice; m < S::kSlices && mine > 0; m += dv.slices) {
-                // a slice lies within one warp's copies, or (steps of 32) spans two warps' 8 positions each
-                uint32_t has = pipe.valid[stage][m * kWarps / S::kSlices];
-                if (S::kSlices < kWarps) has |= pipe.valid[stage][m * kWarps / S::kSlices + 1] << 8;
-                if (has == 0) continue;
-                const bool ok = has >> key & 1;
-                const char* keys = pipe.ring + stage * S::kStage + m * 16 * S::kRow;
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-                for (int d = 0; d < S::DP; d += 4) {
-                    const float4 k = *reinterpret_cast<const float4*>(keys + key * S::kRow + d * 4);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const float4 q = *reinterpret_cast<const float4*>(qs + (qh4 + u) * S::DP + d);
-                        s[u] = fmaf(k.x, q.x, fmaf(k.y, q.y, fmaf(k.z, q.z, fmaf(k.w, q.w, s[u]))));
-                    }
-                }
-                float f[4];
-                bool moved = false;
+        for (int m = dv.slice; m < S::kSlices && mine > 0; m += dv.slices) {
+            const uint32_t has = slice_valid<S, TILED>(sh.valid[pp.stage], m);
+            if (has == 0) continue;
+            const bool ok = has >> key & 1;
+            char* keys = pp.ring + pp.stage * S::kStage + m * 16 * kPanel;
+            if (TILED && has != 0xffffu) clear_rows<S>(keys + S::kHalf, has, lane);
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            constexpr int kSpan = NQ == 8 ? S::DP : S::DP / 2;
+            const int d0 = NQ == 8 ? 0 : half * kSpan;
+#pragma unroll 8
+            for (int d = 0; d < kSpan; d += 4) {
+                const int u4 = (d0 + d) / 4;  // unit of the row
+                const float4 k = *reinterpret_cast<const float4*>(keys + (u4 / 8) * (S::kStep * kPanel) + key * kPanel + ((u4 % 8 ^ (key & 7)) << 4));
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    s[u] = ok ? s[u] * to_log2 : -INFINITY;
-                    float top = s[u];
-#pragma unroll
-                    for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, x));
-                    top = fmaxf(ref[u], top);
-                    f[u] = top == ref[u] ? 1.f : exp2f(ref[u] - top);
-                    moved = moved || f[u] != 1.f;
-                    ref[u] = top;
-                    const float p = exp2f(s[u] - (top == -INFINITY ? 0.f : top));
-                    sum[u] = fmaf(sum[u], f[u], p);
-                    ps[key * 8 + qh4 + u] = p;
+                    const float4 q = *reinterpret_cast<const float4*>(qs + (qh4 + u) * S::DP + d0 + d);
+                    s[u] = fmaf(k.x, q.x, fmaf(k.y, q.y, fmaf(k.z, q.z, fmaf(k.w, q.w, s[u]))));
                 }
-                if (__any_sync(kFull, moved)) {
+            }
+            float f[4];
+            bool moved = false;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float fj = __shfl_sync(kFull, f[j & 3], j < 4 ? 0 : 16);
+            for (int u = 0; u < 4; ++u) {
+                if (NQ == 4) s[u] += __shfl_xor_sync(kFull, s[u], 16);
+                s[u] = ok ? s[u] * to_log2 : -INFINITY;
+                float top = s[u];
 #pragma unroll
-                        for (int i = 0; i < kOwn; ++i) o[j][i] *= fj;
-                    }
+                for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, x));
+                top = fmaxf(ref[u], top);
+                f[u] = top == ref[u] ? 1.f : exp2f(ref[u] - top);
+                moved = moved || f[u] != 1.f;
+                ref[u] = top;
+                const float p = exp2f(s[u] - (top == -INFINITY ? 0.f : top));
+                sum[u] = fmaf(sum[u], f[u], p);
+                if (NQ == 8 || half == 0) ps[key * NQ + qh4 + u] = p;
+            }
+            if (__any_sync(kFull, moved)) {
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) {
+                    const float fj = __shfl_sync(kFull, f[j & 3], j < 4 ? 0 : 16);
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) o[j][i] *= fj;
                 }
-                __syncwarp();
-                const char* vals = keys + S::kHalf;
-#pragma unroll 4
-                for (int p = 0; p < 16; ++p) {
-                    const float4 w0 = *reinterpret_cast<const float4*>(ps + p * 8), w1 = *reinterpret_cast<const float4*>(ps + p * 8 + 4);
+            }
+            __syncwarp();
+            const char* vals = keys + S::kHalf;
+#pragma unroll 8
+            for (int p = 0; p < 16; ++p) {
+                float w[NQ];
 #pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        const float v = *reinterpret_cast<const float*>(vals + p * S::kRow + (lane + 32 * i) * 4);
-                        o[0][i] = fmaf(w0.x, v, o[0][i]);
-                        o[1][i] = fmaf(w0.y, v, o[1][i]);
-                        o[2][i] = fmaf(w0.z, v, o[2][i]);
-                        o[3][i] = fmaf(w0.w, v, o[3][i]);
-                        o[4][i] = fmaf(w1.x, v, o[4][i]);
-                        o[5][i] = fmaf(w1.y, v, o[5][i]);
-                        o[6][i] = fmaf(w1.z, v, o[6][i]);
-                        o[7][i] = fmaf(w1.w, v, o[7][i]);
-                    }
+                for (int j = 0; j < NQ; j += 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(ps + p * NQ + j);
+                    w[j] = x.x;
+                    w[j + 1] = x.y;
+                    w[j + 2] = x.z;
+                    w[j + 3] = x.w;
                 }
-                __syncwarp();
-            }
-            stage = stage + 1 == S::kStages ? 0 : stage + 1;
-        }
-        pipe.stage = stage;
-        // ---- sums over the lanes, then over the slices
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-#pragma unroll
-            for (int x = 1; x < 16; x <<= 1) sum[u] += __shfl_xor_sync(kFull, sum[u], x);
-            if (key == 0) stats[warp][qh4 + u] = float2{ref[u], sum[u]};
-        }
-        __syncthreads();  // also: everyone is done with the last step's stage, which now carries the outputs
-        const int used = stage == 0 ? S::kStages - 1 : stage - 1;
-        float* carry = reinterpret_cast<float*>(pipe.ring + used * S::kStage);
-        float total[8], high[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float top = -INFINITY, all = 0.f;
-            for (int z = 0; z < dv.slices; ++z) top = fmaxf(top, stats[z * dv.groups + dv.group][j].x);
-            for (int z = 0; z < dv.slices; ++z) {
-                const float2 st = stats[z * dv.groups + dv.group][j];
-                all += st.x == -INFINITY ? 0.f * st.y : st.y * (st.x == top ? 1.f : exp2f(st.x - top));
-            }
-            const float own = stats[warp][j].x, fj = own == top ? 1.f : (own == -INFINITY ? 0.f : exp2f(own - top));
-            total[j] = all;
-            high[j] = top;
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) {
-                o[j][i] *= fj;
-                if (dv.slice > 0 && dv.slice < dv.slices)
-                    carry[((dv.slice - 1) * dv.groups + dv.group) * (8 * S::DP) + j * S::DP + lane + 32 * i] = o[j][i];
-            }
-        }
-        __syncthreads();
-        if (dv.slice == 0 && mine > 0) {
-            const bool alone = cur.alone(g.l);
-            const int64_t slot = cur.slot(g.l, worker);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (j >= mine) break;
-                int row, qh;
-                place(q0 + j, &row, &qh);
-                float* out = static_cast<float*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head;
-                const float inv = total[j] == 0.f ? 0.f : 1.f / total[j];
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i) {
-                    const int d = lane + 32 * i;
-                    float x = o[j][i];
-                    for (int z = 1; z < dv.slices; ++z) x += carry[((z - 1) * dv.groups + dv.group) * (8 * S::DP) + j * S::DP + d];
-                    if (d >= g.c.D) continue;
-                    if (alone) out[d] = x * inv;
-                    else g.l.part[(slot + q0 + j) * g.c.D + d] = x;
-                }
-                if (lane == 0) {
-                    if (!alone) g.l.stat[slot + q0 + j] = float2{high[j], total[j]};
-                    else if (g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total[j] == 0.f ? -INFINITY : kLn2 * (high[j] + log2f(total[j]));
+                    const float v = *reinterpret_cast<const float*>(vals + i * (S::kStep * kPanel) + p * kPanel + ((lane >> 2 ^ (p & 7)) << 4) + (lane & 3) * 4);
+#pragma unroll
+                    for (int j = 0; j < NQ; ++j) o[j][i] = fmaf(w[j], v, o[j][i]);
                 }
             }
+            __syncwarp();
         }
-        clear_margin<S>(pipe, used, g.c.D);
-        cur.next_item(g.l);
+        next_stage(pp, S::kStages);
+    }
+    if (index + 1 < feed.items) list_rows(sh.queue[(index + 1) % kQueue].mask, sh.rows[(index + 1) & 1][warp], lane);
+    // ---- sums over the lanes, then over the slices
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) sum[u] += __shfl_xor_sync(kFull, sum[u], x);
+        if (key == 0 && (NQ == 8 || half == 0)) sh.stats[warp][qh4 + u] = float2{ref[u], sum[u]};
+    }
+    __syncthreads();  // also: everyone is done with the last step's stage, which now carries the outputs
+    float* carry = reinterpret_cast<float*>(pp.ring + (pp.stage == 0 ? S::kStages - 1 : pp.stage - 1) * S::kStage);
+    if (mine > 0)
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            float top = -INFINITY;
+            for (int z = 0; z < dv.slices; ++z) top = fmaxf(top, sh.stats[z * dv.groups + dv.group][j].x);
+            const float own = sh.stats[warp][j].x, f = own == top ? 1.f : (own == -INFINITY ? 0.f : exp2f(own - top));
+            if (lane == 0) sh.scaled[warp][j] = sh.stats[warp][j].y * f;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) carry[(warp * 8 + j) * (S::DP + 4) + lane + 32 * i] = o[j][i] * f;
+        }
+    __syncthreads();
+    write_tile<S>(g, it, dv, carry, sh, rows, 0, pp);
+    if (TILED) fence_async_smem();  // before a copy may write there again
+    return true;
+}
+
+template <class S, bool TILED>
+__global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_f32_kernel(const __grid_constant__ AttendArgs g) {
+    extern __shared__ __align__(1024) char smem[];
+    __shared__ Shared<S> sh;
+    static_assert(sizeof(sh) <= S::kBeside, "beside the ring");
+    Pipe pp;
+    Feeder<S, TILED> feed;
+    if (!open_pipe<S, TILED>(g, smem, pp, sh, feed)) return;
+    float* qs = reinterpret_cast<float*>(pp.ring + S::kStages * S::kStage) + pp.warp * (8 * S::DP + 16 * 8);  // [8][DP]
+    float* ps = qs + 8 * S::DP;                                                                               // [16][8]
+    list_rows(sh.queue[0].mask, sh.rows[0][pp.warp], pp.lane);
+    fill_pipe<S, TILED>(g, pp, sh, feed);
+    for (int index = 0; index < feed.items; ++index) {
+        const Item it = sh.queue[index % kQueue];
+        const bool ok = it.nq <= 4 ? run_item_f32<S, TILED, 4>(g, it, qs, ps, feed, pp, sh, index)
+                                   : run_item_f32<S, TILED, 8>(g, it, qs, ps, feed, pp, sh, index);
+        if (!ok) {
+            give_up<S>(g, pp, sh);
+            return;
+        }
     }
 }
 
@@ -1130,7 +1368,7 @@ constexpr int kMaxWorkers = 2 * kSMs;
 constexpr int kJoinThreads = 128;
 
 template <int DT, int WPQ>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const AttendArgs g) {
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ AttendArgs g) {
     using T = typename PoolIo<DT>::type;
     constexpr int kJoinWarps = kJoinThreads / 32, kQueries = kJoinWarps / WPQ, kOwn = kMaxHeadDim / 128, kList = 32, kBatch = 8;
     __shared__ int64_t slots[kJoinWarps][kList];
@@ -1203,9 +1441,9 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const AttendAr
             with &= with - 1;
             const int qi = __popc(sg.mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / qt_size;
             const int steps = steps_of(ls, sg.p0, sg.p1);
-            const int w = step_cost(ls, min(qt_size, __popc(sg.mask) * ls.ratio - qt * qt_size));
-            const int64_t a = b.before + head * tp.cost + sg.start + (int64_t)qt * steps * step_cost(ls, qt_size);
-            const int64_t k0 = a / b.share, k1 = (a + (int64_t)steps * w - 1) / b.share;
+            const int w = step_cost(ls.group, min(qt_size, __popc(sg.mask) * ls.ratio - qt * qt_size));
+            const int64_t a = b.before + head * tp.cost + sg.start + (int64_t)qt * steps * step_cost(ls.group, qt_size);
+            const int64_t k0 = quotient(a, b.share), k1 = quotient(a + (int64_t)steps * w - 1, b.share);
             const int64_t first = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio) + (int64_t)sg.before * ls.ratio + qi;
             for (int64_t kb = k0; kb <= k1; kb += 32) {
                 const int64_t k = kb + lane;
@@ -1256,10 +1494,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const AttendAr
     for (int i = 0; i < kOwn; ++i) {
         const int d = lane * 4 + i * 128;
         if (d >= g.c.D) continue;
-        put(out + d, o[i].x * inv);
-        put(out + d + 1, o[i].y * inv);
-        put(out + d + 2, o[i].z * inv);
-        put(out + d + 3, o[i].w * inv);
+        put4(out + d, float4{o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv});
     }
     if (lane == 0 && g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total == 0.f ? -INFINITY : kLn2 * (top + log2f(total));
 }
@@ -1284,6 +1519,29 @@ Scratch scratch_of(int R, int Hq, int D) {
     return s;
 }
 
+// A pool as a tensor of three dimensions for tiled copies of 16 positions x 128 bytes, swizzled; components beyond the head
+// read as zero.
+bool tile_map(CUtensorMap* map, const PagedView& c, const char* pool) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            fn = nullptr;
+        return reinterpret_cast<Encode>(fn);
+    }();
+    if (!encode) return false;
+    const int elem = c.dt == PSMC_F32 ? 4 : (c.dt == PSMC_BF16 ? 2 : 1);
+    const CUtensorMapDataType type = c.dt == PSMC_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                                      : (c.dt == PSMC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8);
+    const cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.H * c.block_len, (cuuint64_t)c.n_blocks};
+    const cuuint64_t strides[2] = {(cuuint64_t)c.D * elem, (cuuint64_t)c.blk_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)(kPanel / elem), 16, 1}, unit[3] = {1, 1, 1};
+    return encode(map, type, 3, const_cast<char*>(pool), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DT, int DP>
 cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream) {
     using S = Shape<DT, DP>;
@@ -1305,9 +1563,11 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.l.workers = S::kCtas * kSMs;
     cudaError_t e = launch_chained(paged_plan_kernel, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
     if (e != cudaSuccess) return e;
+    const bool tiled = c.block_len % 16 == 0;
+    if (tiled && (!tile_map(&g.k_map, c, c.k) || !tile_map(&g.v_map, c, c.v))) return cudaErrorInvalidValue;
     void (*fn)(const AttendArgs);
-    if constexpr (DT == PSMC_F32) fn = paged_attend_f32_kernel<S>;
-    else fn = paged_attend_kernel<S>;
+    if constexpr (DT == PSMC_F32) fn = tiled ? paged_attend_f32_kernel<S, true> : paged_attend_f32_kernel<S, false>;
+    else fn = tiled ? paged_attend_kernel<S, true> : paged_attend_kernel<S, false>;
     e = allow_dynamic_smem(reinterpret_cast<const void*>(fn), S::kBytes);
     if (e == cudaSuccess) e = launch_chained(fn, dim3((unsigned)g.l.workers), dim3(kWarps * 32), S::kBytes, stream, g);
     if (e != cudaSuccess) return e;
