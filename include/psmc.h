@@ -344,7 +344,7 @@ psmc_status psmc_rope_frequencies(psmc_rope_scaling kind, int rot_dim, double th
 /* n tokens: token i is position positions[i] of row rows[i] (both DEVICE; rows NULL: row i, n <= R).  Its keys k [n, H, D]
  * get their rotary positions (rope NULL: none) and go into the cache with its values v; its queries q [n, Hq, D], when
  * given, get theirs into q_out, which may be q itself.  Angles are formed in 64 bits.  Tokens with rows[i] < 0 are padding, and
- * tokens of rows with skip[row] != 0 (DEVICE [R], may be NULL) are left out: nothing of theirs is read or written.
+ * tokens of rows with skip[row] != 0 (DEVICE [R], may be NULL) are left out: nothing of theirs is written.
  * The block of a position must belong to the row alone or be written by one of its owners only; a position that appears
  * twice in a call gets one of the two tokens. */
 psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows, const int32_t* positions,

@@ -55,10 +55,6 @@ class RopeDesc(C.Structure):
     _fields_ = [("freqs", C.c_void_p), ("rot_dim", C.c_int), ("layout", C.c_int), ("mscale", C.c_double)]
 
 
-class Heads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
-
-
 def lib():
     """Load libpsmc.so (once).  Raises if it has not been built: there is no other code path."""
     global _lib
@@ -125,19 +121,19 @@ def lib():
         for name in ("psmc_kv_paged_table", "psmc_kv_paged_refcount", "psmc_kv_paged_free_count"):
             getattr(L, name).restype = C.c_void_p
             getattr(L, name).argtypes = [vp]
-        hp, ip = C.POINTER(Heads), C.c_int
+        hp, ip = vp, C.c_int  # psmc_heads: addresses within one array of a call's heads
         L.psmc_paged_block_bytes.restype = C.c_size_t
         L.psmc_paged_block_bytes.argtypes = [ip, ip, ip, ip]
         L.psmc_rope_frequencies.restype = ip
         L.psmc_rope_frequencies.argtypes = [ip, ip, C.c_double, C.c_double, C.c_double, C.c_double, ip, vp, vp]
         L.psmc_paged_write.restype = ip
-        L.psmc_paged_write.argtypes = [C.POINTER(PagedKvDesc), ip, vp, vp, vp, C.POINTER(RopeDesc), hp, hp, ip, hp, hp, vp, vp]
+        L.psmc_paged_write.argtypes = [vp, ip, vp, vp, vp, C.POINTER(RopeDesc), hp, hp, ip, hp, hp, vp, vp]
         L.psmc_paged_attend_scratch_bytes.restype = C.c_size_t
         L.psmc_paged_attend_scratch_bytes.argtypes = [ip, ip, ip, ip]
         L.psmc_paged_attend.restype = ip
-        L.psmc_paged_attend.argtypes = [C.POINTER(PagedKvDesc), vp, ip, vp, ip, hp, hp, C.c_float, vp, vp, C.c_size_t, vp, vp]
+        L.psmc_paged_attend.argtypes = [vp, vp, ip, vp, ip, hp, hp, C.c_float, vp, vp, C.c_size_t, vp, vp]
         L.psmc_paged_read.restype = ip
-        L.psmc_paged_read.argtypes = [C.POINTER(PagedKvDesc), vp, vp, vp, vp, ip, C.c_int64, C.c_int64, vp, vp]
+        L.psmc_paged_read.argtypes = [vp, vp, vp, vp, vp, ip, C.c_int64, C.c_int64, vp, vp]
         L.psmc_kv_paged_write.restype = ip
         L.psmc_kv_paged_write.argtypes = [vp, C.POINTER(KvPools), ip, ip, vp, vp, C.POINTER(RopeDesc), hp, hp, ip, hp, hp, vp]
         L.psmc_kv_paged_attend.restype = ip
@@ -396,41 +392,38 @@ class Psmc:
                        positions: torch.Tensor = None, stream=None):
         """psmc_kv_paged_write: the next token of every live row (k, v [R, H, D], q [R, Hq, D]), or with rows and positions
         (int32 [n]) any tokens.  Returns q_out (q with its rotary positions), allocated if not given."""
-        n = k.shape[0]
-        io = _check_kv_tokens(pools.dt, pools.n_kv_heads, pools.head_dim, n, k, v)
+        n, dev = k.shape[0], k.get_device()
         if rows is None:
             assert positions is None and n == self.R
         else:
-            _check_ints(rows, n, k.device)
-            _check_ints(positions, n, k.device)
-        q_out = _check_queries(q, q_out, n, pools.head_dim, io, k.device, stream)
-        _on_device(k.device, lambda: _check(lib().psmc_kv_paged_write(
-            self._h, C.byref(pools), layer, n, _ptr(rows), _ptr(positions), _ref(rope), _heads(k), _heads(v),
-            0 if q is None else q.shape[1], _heads(q), _heads(q_out), _stream(stream)), "psmc_kv_paged_write"))
+            _check_ints(rows, n, dev)
+            _check_ints(positions, n, dev)
+        heads, q_out = _write_heads(k, v, q, q_out, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, stream)
+        at = C.addressof(heads)
+        _launch(dev, "psmc_kv_paged_write", self._h, C.byref(pools), layer, n, _ptr(rows), _ptr(positions), _ref(rope), at, at + 24,
+                0 if q is None else q.shape[1], 0 if q is None else at + 48, 0 if q is None else at + 72, _raw_stream(stream, dev))
         return q_out
 
     def kv_paged_attend(self, pools: KvPools, layer: int, q: torch.Tensor, scale: float, out: torch.Tensor = None,
                         lse: torch.Tensor = None, scratch: torch.Tensor = None, stream=None):
         """psmc_kv_paged_attend: q [R, Hq, D] of every row's new token over its len + 1 positions (finished rows of out and
         lse are left as they were; zeros in an out allocated here)."""
-        io = _check_queries_shape(q, self.R, pools.n_kv_heads, pools.head_dim, pools.dt)
-        if out is None:
-            with _allocate_on(stream):
-                out = torch.zeros_like(q)
-        _check_out(q, out, io)
-        _check_lse(lse, q)
-        scratch = _attend_scratch(scratch, self.R, q.shape[1], pools.n_kv_heads, pools.head_dim, q.device, stream)
-        _on_device(q.device, lambda: _check(lib().psmc_kv_paged_attend(
-            self._h, C.byref(pools), layer, q.shape[1], _heads(q), _heads(out), scale, _ptr(lse), scratch.data_ptr(),
-            scratch.numel(), _stream(stream)), "psmc_kv_paged_attend"))
+        dev = q.get_device()
+        heads, out = _attend_heads(q, out, lse, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, True, stream)
+        need = lib().psmc_paged_attend_scratch_bytes(self.R, q.shape[1], pools.n_kv_heads, pools.head_dim)
+        scratch = _scratch(scratch, need, dev, stream)
+        at = C.addressof(heads)
+        _launch(dev, "psmc_kv_paged_attend", self._h, C.byref(pools), layer, q.shape[1], at, at + 24, scale, _ptr(lse),
+                scratch.data_ptr(), scratch.numel(), _raw_stream(stream, dev))
         return out
 
     def kv_paged_read(self, pools: KvPools, layer: int, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
         """psmc_kv_paged_read: the live positions of every row into dense [R, H, max_len, D] tensors."""
-        d = _check_dense(k_out, v_out, self.R, pools.n_kv_heads, pools.head_dim, pools.dt)
-        _on_device(d.device, lambda: _check(lib().psmc_kv_paged_read(
-            self._h, C.byref(pools), layer, _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0), d.stride(1),
-            _stream(stream)), "psmc_kv_paged_read"))
+        d = k_out if k_out is not None else v_out
+        dev = d.get_device()
+        _check_dense(k_out, v_out, d, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev)
+        _launch(dev, "psmc_kv_paged_read", self._h, C.byref(pools), layer, _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0),
+                d.stride(1), _raw_stream(stream, dev))
 
     def reindex_kv_paged(self, pools: KvPools, stream=None):
         _check(lib().psmc_reindex_kv_paged(self._h, C.byref(pools), _stream(stream)), "psmc_reindex_kv_paged")
@@ -555,15 +548,29 @@ class PagedKv(PagedKvDesc):
         super().__init__(k.data_ptr(), v.data_ptr(), table.data_ptr(), table.stride(0), table.shape[0], k.shape[0], block_len,
                          table.shape[1], n_kv_heads, head_dim, dt)
         self._keep = (k, v, table)
-        self.device = k.device
+        self.index, self.io = k.get_device(), _io_dtype(dt)
 
 
-def _on_device(device, call):
-    """Launches belong to the device of their tensors, whichever is current."""
-    if device.index == torch.cuda.current_device():
-        return call()
-    with torch.cuda.device(device):
-        return call()
+# A decode loop makes two of these calls per layer and token, on small tensors: what happens on the host is kept short.
+_HeadsArray = C.c_int64 * 12  # up to four psmc_heads: {address, row stride, head stride}
+
+
+def _launch(index: int, name: str, *args) -> None:
+    """Calls the library with the tensors' device current, whichever is."""
+    fn = getattr(lib(), name)
+    if index == torch.cuda.current_device():
+        code = fn(*args)
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args)
+    if code != OK:
+        raise PsmcError(code, name)
+
+
+def _raw_stream(stream, index: int) -> int:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _allocate_on(stream):
@@ -577,81 +584,70 @@ def _ref(desc):
     return None if desc is None else C.byref(desc)
 
 
-def _heads(t):
-    return None if t is None else C.byref(Heads(t.data_ptr(), t.stride(0), t.stride(1)))
-
-
 def _io_dtype(dtype_code: int):
     return torch.float32 if dtype_code == F32 else torch.bfloat16
 
 
-def _check_kv_tokens(dtype_code, H, D, n, k, v):
-    io = _io_dtype(dtype_code)
-    for t in (k, v):
-        assert t.is_cuda and t.dtype == io and t.shape == (n, H, D) and t.stride(2) == 1 and t.device == k.device
-    return io
+def _check_heads(t, shape, io, index):
+    assert t.shape == shape and t.dtype is io and t.get_device() == index and t.stride(2) == 1
 
 
-def _check_queries(q, q_out, n, D, io, device, stream):
+def _write_heads(k, v, q, q_out, H, D, io, index, stream):
+    assert index >= 0
+    n = k.shape[0]
+    _check_heads(k, (n, H, D), io, index)
+    _check_heads(v, (n, H, D), io, index)
     if q is None:
         assert q_out is None
-        return None
+        return _HeadsArray(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1)), None
     if q_out is None:
         with _allocate_on(stream):
             q_out = torch.empty_like(q)
-    for t in (q, q_out):
-        assert t.device == device and t.dtype == io and t.dim() == 3 and t.shape == q.shape and t.stride(2) == 1
-    assert q.shape[0] == n and q.shape[2] == D
-    return q_out
+    shape = (n, q.shape[1], D)
+    _check_heads(q, shape, io, index)
+    _check_heads(q_out, shape, io, index)
+    return _HeadsArray(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), q.data_ptr(), q.stride(0),
+                       q.stride(1), q_out.data_ptr(), q_out.stride(0), q_out.stride(1)), q_out
 
 
-def _check_queries_shape(q, R, H, D, dtype_code):
-    io = _io_dtype(dtype_code)
-    assert q.is_cuda and q.dtype == io and q.dim() == 3 and q.stride(2) == 1
-    assert q.shape[0] == R and q.shape[2] == D and q.shape[1] % H == 0
-    return io
-
-
-def _check_out(q, out, io):
-    assert out.device == q.device and out.dtype == io and out.shape == q.shape and out.stride(2) == 1
-
-
-def _check_lse(lse, q):
+def _attend_heads(q, out, lse, R, H, D, io, index, zeros, stream):
+    assert index >= 0 and q.dim() == 3 and q.shape[1] % H == 0
+    shape = (R, q.shape[1], D)
+    _check_heads(q, shape, io, index)
+    if out is None:
+        with _allocate_on(stream):
+            out = torch.zeros_like(q) if zeros else torch.empty_like(q)
+    _check_heads(out, shape, io, index)
     if lse is not None:
-        assert lse.device == q.device and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
+        assert lse.get_device() == index and lse.dtype is torch.float32 and lse.is_contiguous() and lse.shape == shape[:2]
+    return _HeadsArray(q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1)), out
 
 
-def _check_ints(t, n, device):
-    assert t is not None and t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n
+def _check_ints(t, n, index):
+    assert t is not None and t.get_device() == index and t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous()
 
 
-def _check_skip(skip, R, device):
+def _check_optional(skip, status_word, R, index):
     if skip is not None:
-        assert skip.device == device and skip.dtype == torch.uint8 and skip.is_contiguous() and skip.numel() == R
+        assert skip.get_device() == index and skip.dtype is torch.uint8 and skip.shape == (R,) and skip.is_contiguous()
+    if status_word is not None:
+        assert status_word.get_device() == index and status_word.dtype is torch.int32 and status_word.numel() >= 1
 
 
-def _check_word(word, device):
-    if word is not None:
-        assert word.device == device and word.dtype == torch.int32 and word.numel() >= 1
-
-
-def _check_dense(k_out, v_out, R, H, D, dtype_code):
-    d = k_out if k_out is not None else v_out
+def _check_dense(k_out, v_out, d, R, H, D, io, index):
+    assert index >= 0
     for t in (k_out, v_out):
         if t is not None:
-            assert t.is_cuda and t.dtype == _io_dtype(dtype_code) and t.dim() == 4 and t.device == d.device
-            assert t.shape == d.shape and t.stride() == d.stride()
-    assert d.shape[0] == R and d.shape[1] == H and d.shape[3] == D and d.stride(3) == 1 and d.stride(2) == D
-    return d
+            assert t.get_device() == index and t.dtype is io and t.shape == d.shape and t.stride() == d.stride()
+    assert d.dim() == 4 and d.shape[0] == R and d.shape[1] == H and d.shape[3] == D and d.stride(3) == 1 and d.stride(2) == D
 
 
-def _attend_scratch(scratch, R, Hq, H, D, device, stream):
+def _scratch(scratch, need, index, stream):
     """Workspace of one call: the caller's, or a fresh one (from the graph's own pool while one is captured)."""
-    need = lib().psmc_paged_attend_scratch_bytes(R, Hq, H, D)
     if scratch is None:
         with _allocate_on(stream):
-            scratch = torch.empty(need, dtype=torch.uint8, device=device)
-    assert scratch.device == device and scratch.dtype == torch.uint8 and scratch.is_contiguous() and scratch.numel() >= need
+            return torch.empty(need, dtype=torch.uint8, device=index)
+    assert scratch.get_device() == index and scratch.dtype is torch.uint8 and scratch.is_contiguous() and scratch.numel() >= need
     return scratch
 
 
@@ -660,18 +656,16 @@ def paged_write(cache: PagedKv, k: torch.Tensor, v: torch.Tensor, rows, position
                 stream=None):
     """psmc_paged_write: k, v [n, H, D] (and q [n, Hq, D]) of tokens at positions[i] of rows[i] (int32; rows None: row i).
     Returns q_out (q with its rotary positions), allocated if not given."""
-    n, dev = k.shape[0], cache.device
-    io = _check_kv_tokens(cache.dt, cache.n_kv_heads, cache.head_dim, n, k, v)
-    assert k.device == dev
+    n, dev = k.shape[0], cache.index
     if rows is not None:
         _check_ints(rows, n, dev)
     _check_ints(positions, n, dev)
-    _check_skip(skip, cache.R, dev)
-    _check_word(status_word, dev)
-    q_out = _check_queries(q, q_out, n, cache.head_dim, io, dev, stream)
-    _on_device(dev, lambda: _check(lib().psmc_paged_write(
-        C.byref(cache), n, _ptr(rows), positions.data_ptr(), _ptr(skip), _ref(rope), _heads(k), _heads(v),
-        0 if q is None else q.shape[1], _heads(q), _heads(q_out), _ptr(status_word), _stream(stream)), "psmc_paged_write"))
+    _check_optional(skip, status_word, cache.R, dev)
+    heads, q_out = _write_heads(k, v, q, q_out, cache.n_kv_heads, cache.head_dim, cache.io, dev, stream)
+    at = C.addressof(heads)
+    _launch(dev, "psmc_paged_write", C.addressof(cache), n, _ptr(rows), positions.data_ptr(), _ptr(skip), _ref(rope), at, at + 24,
+            0 if q is None else q.shape[1], 0 if q is None else at + 48, 0 if q is None else at + 72, _ptr(status_word),
+            _raw_stream(stream, dev))
     return q_out
 
 
@@ -680,36 +674,28 @@ def paged_attend(cache: PagedKv, q: torch.Tensor, lens: torch.Tensor, scale: flo
                  status_word: torch.Tensor = None, stream=None) -> torch.Tensor:
     """psmc_paged_attend: q [R, Hq, D], one token per row, over positions 0 .. lens[r] + extra of the row (lens int32 [R]).
     lse: float32 [R, Hq] or None.  Rows with skip != 0 are left as they were (zeros in an out allocated here)."""
-    dev = cache.device
-    io = _check_queries_shape(q, cache.R, cache.n_kv_heads, cache.head_dim, cache.dt)
-    assert q.device == dev
-    _check_ints(lens, cache.R, dev)
-    _check_skip(skip, cache.R, dev)
-    _check_word(status_word, dev)
-    _check_lse(lse, q)
-    if out is None:
-        with _allocate_on(stream):
-            out = torch.empty_like(q) if skip is None else torch.zeros_like(q)
-    _check_out(q, out, io)
-    scratch = _attend_scratch(scratch, cache.R, q.shape[1], cache.n_kv_heads, cache.head_dim, dev, stream)
-    _on_device(dev, lambda: _check(lib().psmc_paged_attend(
-        C.byref(cache), lens.data_ptr(), extra, _ptr(skip), q.shape[1], _heads(q), _heads(out), scale, _ptr(lse),
-        scratch.data_ptr(), scratch.numel(), _ptr(status_word), _stream(stream)), "psmc_paged_attend"))
+    dev, R, H, D = cache.index, cache.R, cache.n_kv_heads, cache.head_dim
+    _check_ints(lens, R, dev)
+    _check_optional(skip, status_word, R, dev)
+    heads, out = _attend_heads(q, out, lse, R, H, D, cache.io, dev, skip is not None, stream)
+    Hq = q.shape[1]
+    scratch = _scratch(scratch, lib().psmc_paged_attend_scratch_bytes(R, Hq, H, D), dev, stream)
+    at = C.addressof(heads)
+    _launch(dev, "psmc_paged_attend", C.addressof(cache), lens.data_ptr(), extra, _ptr(skip), Hq, at, at + 24, scale, _ptr(lse),
+            scratch.data_ptr(), scratch.numel(), _ptr(status_word), _raw_stream(stream, dev))
     return out
 
 
 def paged_read(cache: PagedKv, lens: torch.Tensor, k_out: torch.Tensor = None, v_out: torch.Tensor = None,
                skip: torch.Tensor = None, status_word: torch.Tensor = None, stream=None) -> None:
     """psmc_paged_read: positions 0 .. lens[r] of every row into dense [R, H, max_len, D] tensors (one of them may be None)."""
-    dev = cache.device
-    d = _check_dense(k_out, v_out, cache.R, cache.n_kv_heads, cache.head_dim, cache.dt)
-    assert d.device == dev
+    dev = cache.index
+    d = k_out if k_out is not None else v_out
+    _check_dense(k_out, v_out, d, cache.R, cache.n_kv_heads, cache.head_dim, cache.io, dev)
     _check_ints(lens, cache.R, dev)
-    _check_skip(skip, cache.R, dev)
-    _check_word(status_word, dev)
-    _on_device(dev, lambda: _check(lib().psmc_paged_read(
-        C.byref(cache), lens.data_ptr(), _ptr(skip), _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0), d.stride(1),
-        _ptr(status_word), _stream(stream)), "psmc_paged_read"))
+    _check_optional(skip, status_word, cache.R, dev)
+    _launch(dev, "psmc_paged_read", C.addressof(cache), lens.data_ptr(), _ptr(skip), _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0),
+            d.stride(1), _ptr(status_word), _raw_stream(stream, dev))
 
 
 def logits_pass_scratch_bytes(R: int, V: int) -> int:

@@ -667,9 +667,9 @@ psmc_status paged_write(const PagedView& c, int n, const int32_t* rows, const in
     if (!rows && n > c.R) return PSMC_E_INVAL;
     PagedWrite w{};
     w.n = n; w.rows = rows; w.positions = positions; w.skip = skip; w.status = status;
-    w.k_in = heads_view(k); w.v_in = heads_view(v);
+    w.in[1] = heads_view(k); w.in[2] = heads_view(v);
     if (q) {
-        w.q = true; w.Hq = Hq; w.q_in = heads_view(q); w.q_out = heads_view(q_out);
+        w.q = true; w.Hq = Hq; w.in[0] = heads_view(q); w.q_out = heads_view(q_out);
     }
     w.mscale = 1.f;
     if (rope) {

@@ -217,9 +217,9 @@ struct PagedWrite {
     const double* freqs;       // [rot / 2]
     int rot, pairs;
     float mscale;
-    int lanes_per_head;        // set by the launch
-    HeadsView k_in, v_in, q_in, q_out;
-    bool q;                    // q_in / q_out are given
+    int lanes_per_head, warps_per_token;  // set by the launch
+    HeadsView in[3], q_out;    // in: queries, keys, values
+    bool q;                    // in[0] and q_out are given
     int32_t* status;
 };
 cudaError_t launch_paged_write(const PagedView& c, const PagedWrite& w, cudaStream_t stream);

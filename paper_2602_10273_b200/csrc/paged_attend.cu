@@ -427,17 +427,6 @@ struct Walk {
 };
 
 // ------------------------------------------------------------------------------------------------- copies and matrix tiles
-struct FastDiv {         // division of numbers below 2^31 by d
-    uint32_t mul;
-    int shift;
-};
-FastDiv fast_div(int d) {
-    int l = 0;
-    while ((int64_t)1 << l < d) ++l;
-    return FastDiv{(uint32_t)(((((uint64_t)1 << l) - d) << 32) / d + 1), l};
-}
-__device__ __forceinline__ int div_by(int x, const FastDiv& f) { return (int)((__umulhi((uint32_t)x, f.mul) + (uint32_t)x) >> f.shift); }
-
 __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // 16 bytes, or 16 zero bytes where bytes == 0 (src is then not read)
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {

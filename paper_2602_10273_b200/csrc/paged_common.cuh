@@ -39,6 +39,17 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
+struct FastDiv {         // division of numbers below 2^31 by d
+    uint32_t mul;
+    int shift;
+};
+inline FastDiv fast_div(int d) {
+    int l = 0;
+    while ((int64_t)1 << l < d) ++l;
+    return FastDiv{(uint32_t)(((((uint64_t)1 << l) - d) << 32) / d + 1), l};
+}
+__device__ __forceinline__ int div_by(int x, const FastDiv& f) { return (int)((__umulhi((uint32_t)x, f.mul) + (uint32_t)x) >> f.shift); }
+
 // VEC consecutive elements of type T as one aligned access
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Chunk {
@@ -58,11 +69,6 @@ __device__ __forceinline__ float code_value(uint8_t code) {
     const __half_raw h = __nv_cvt_fp8_to_halfraw(code, __NV_E4M3);
     return __half2float(__half(h));
 }
-// nearest code, ties to even, saturating; a non-finite component becomes the NaN code
-__device__ __forceinline__ uint8_t code_of(float y) {
-    return isfinite(y) ? (uint8_t)__nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3) : (uint8_t)0x7f;
-}
-
 // The block of position p of row r, or -1: outside the table, or an entry that names no block.
 __device__ __forceinline__ int block_of(const PagedView& c, int r, int j) {
     if (j < 0 || j >= c.max_blocks) return -1;

@@ -9,41 +9,60 @@ namespace {
 constexpr int kReadThreads = 256;
 
 template <int DT, int VEC>
-__global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const PagedView c, const PagedRead a) {
+__global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const PagedView c, const PagedRead a, const FastDiv by_access,
+                                                                  const FastDiv by_block) {
     using T = typename PoolIo<DT>::type;
     chain_begin();
     const int which = a.k && a.v ? (int)(blockIdx.y & 1) : (a.k ? 0 : 1);
     const int r = a.k && a.v ? (int)(blockIdx.y >> 1) : (int)blockIdx.y, j = blockIdx.x;
+    const int named = __ldg(c.table + (int64_t)r * c.table_ld + j);  // (asked for together with the length)
+    int64_t n = __ldg(a.lens + r);
     if (a.skip && a.skip[r]) return;
-    int n = __ldg(a.lens + r);
-    if (n > a.max_len || n > c.max_blocks * (int64_t)c.block_len) {
+    const int64_t room = min((int64_t)a.max_len, c.max_blocks * (int64_t)c.block_len);
+    if (n > room) {
         if (j == 0 && threadIdx.x == 0) raise_status(a.status, PSMC_E_STATE);
-        n = (int)min((int64_t)a.max_len, c.max_blocks * (int64_t)c.block_len);
+        n = room;
     }
     const int64_t p0 = (int64_t)j * c.block_len;
     if (p0 >= n) return;
     const int live = (int)min((int64_t)c.block_len, n - p0);
-    const int blk = block_of(c, r, j);
-    if (blk < 0) {
+    if (named < 0 || named >= c.n_blocks) {
         if (threadIdx.x == 0) raise_status(a.status, PSMC_E_STATE);
         return;
     }
-    const char* pool = (which ? c.v : c.k) + (int64_t)blk * c.blk_bytes;
+    const char* pool = (which ? c.v : c.k) + (int64_t)named * c.blk_bytes;
     T* dst = static_cast<T*>(which ? a.v : a.k) + (int64_t)r * a.stride_row + p0 * c.D;
-    const int per_pos = c.D / VEC, per_head = live * per_pos;
-    for (int e = threadIdx.x; e < per_head * c.H; e += kReadThreads) {
-        const int h = e / per_head, x = e - h * per_head, o = x / per_pos, d = (x - o * per_pos) * VEC;
-        const int64_t from = ((int64_t)h * c.block_len + o) * c.D + d;
-        Chunk<T, VEC> out;
-        if (DT == PSMC_F8) {
-            const Chunk<uint8_t, VEC> in = *reinterpret_cast<const Chunk<uint8_t, VEC>*>(pool + from);
-            const float scale = pow2i((int)reinterpret_cast<const uint8_t*>(pool)[c.scale_at + (int64_t)h * c.block_len + o] - 127);
+    const int per_pos = c.D / VEC, total = c.H * c.block_len * per_pos;
+    // Four accesses under way per thread, then their stores (a plain loop of load and store waits for every load by itself).
+    constexpr int kBatch = 4;
+    for (int e0 = threadIdx.x; e0 < total; e0 += kBatch * kReadThreads) {
+        Chunk<T, VEC> wide[kBatch];
+        Chunk<uint8_t, VEC> codes[kBatch];
+        uint8_t scale[kBatch];
+        int64_t to[kBatch];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) out.x[i] = from_float<T>(code_value(in.x[i]) * scale);
-        } else {
-            out = *reinterpret_cast<const Chunk<T, VEC>*>(pool + from * sizeof(T));
+        for (int u = 0; u < kBatch; ++u) {
+            const int e = e0 + u * kReadThreads, x = div_by(e, by_access), d = (e - x * per_pos) * VEC, h = div_by(x, by_block), o = x - h * c.block_len;
+            to[u] = -1;
+            if (e >= total || o >= live) continue;
+            to[u] = (int64_t)h * a.stride_head + (int64_t)o * c.D + d;
+            if (DT == PSMC_F8) {
+                codes[u] = *reinterpret_cast<const Chunk<uint8_t, VEC>*>(pool + (int64_t)x * c.D + d);
+                scale[u] = reinterpret_cast<const uint8_t*>(pool)[c.scale_at + x];
+            } else {
+                wide[u] = *reinterpret_cast<const Chunk<T, VEC>*>(pool + ((int64_t)x * c.D + d) * sizeof(T));
+            }
         }
-        *reinterpret_cast<Chunk<T, VEC>*>(dst + (int64_t)h * a.stride_head + (int64_t)o * c.D + d) = out;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (to[u] < 0) continue;
+            if (DT == PSMC_F8) {
+                const float s = pow2i((int)scale[u] - 127);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) wide[u].x[i] = from_float<T>(code_value(codes[u].x[i]) * s);
+            }
+            *reinterpret_cast<Chunk<T, VEC>*>(dst + to[u]) = wide[u];
+        }
     }
 }
 
@@ -54,7 +73,9 @@ cudaError_t launch(const PagedView& c, const PagedRead& a, cudaStream_t stream) 
     uint64_t bits = (uint64_t)(a.stride_row * sizeof(T)) | (uint64_t)(a.stride_head * sizeof(T)) | (uint64_t)(uintptr_t)a.k |
                     (uint64_t)(uintptr_t)a.v;
     // 16 bytes per access where every destination row starts on such a boundary, else one element
-    auto fn = bits % 16 == 0 && c.D % kFullVec == 0 ? paged_read_kernel<DT, kFullVec> : paged_read_kernel<DT, 1>;
+    const int vec = bits % 16 == 0 && c.D % kFullVec == 0 ? kFullVec : 1;
+    auto fn = vec == kFullVec ? paged_read_kernel<DT, kFullVec> : paged_read_kernel<DT, 1>;
+    const FastDiv by_access = fast_div(c.D / vec), by_block = fast_div(c.block_len);
     const int rows_per_launch = 1 << 14;  // grid.y limit
     const int64_t max_pos = c.max_blocks * (int64_t)c.block_len < a.max_len ? c.max_blocks * (int64_t)c.block_len : a.max_len;
     const unsigned blocks = (unsigned)((max_pos + c.block_len - 1) / c.block_len);
@@ -67,7 +88,8 @@ cudaError_t launch(const PagedView& c, const PagedRead& a, cudaStream_t stream) 
         if (a.skip) aa.skip = a.skip + r0;
         if (a.k) aa.k = static_cast<T*>(a.k) + (int64_t)r0 * a.stride_row;
         if (a.v) aa.v = static_cast<T*>(a.v) + (int64_t)r0 * a.stride_row;
-        const cudaError_t e = launch_chained(fn, dim3(blocks, (unsigned)cc.R * (a.k && a.v ? 2 : 1)), dim3(kReadThreads), 0, stream, cc, aa);
+        const cudaError_t e = launch_chained(fn, dim3(blocks, (unsigned)cc.R * (a.k && a.v ? 2 : 1)), dim3(kReadThreads), 0, stream, cc, aa,
+                                             by_access, by_block);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

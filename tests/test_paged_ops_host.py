@@ -27,6 +27,14 @@ def _kv(B, **over):
     return B.PagedKvDesc(*[f[n] for n, _ in B.PagedKvDesc._fields_])
 
 
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
+
+
+def _heads(data, row, head):
+    return Heads(data, row, head)
+
+
 BAD_KV = [dict(k=0), dict(v=0), dict(table=0), dict(table_ld=3), dict(R=0), dict(n_blocks=0), dict(block_len=0),
           dict(max_blocks=0), dict(n_kv_heads=0), dict(head_dim=0), dict(head_dim=264), dict(head_dim=20),
           dict(dt=3), dict(dt=-1), dict(k=(1 << 20) + 8), dict(v=(1 << 20) + 2), dict(table=(1 << 20) + 2),
@@ -36,7 +44,7 @@ BAD_KV = [dict(k=0), dict(v=0), dict(table=0), dict(table_ld=3), dict(R=0), dict
 
 @pytest.mark.parametrize("bad", BAD_KV, ids=lambda d: ",".join("%s=%s" % i for i in d.items()))
 def test_a_bad_cache_is_refused_by_every_operator(B, bad):
-    L, kv, h = B.lib(), _kv(B, **bad), B.Heads(4 << 20, 128, 64)
+    L, kv, h = B.lib(), _kv(B, **bad), _heads(4 << 20, 128, 64)
     r = C.byref
     assert L.psmc_paged_write(r(kv), 1, 0, 1 << 20, 0, None, r(h), r(h), 0, None, None, 0, 0) == B.E_INVAL
     assert L.psmc_paged_attend(r(kv), 1 << 20, 0, 0, 4, r(h), r(h), 1.0, 0, 1 << 20, 1 << 40, 0, 0) == B.E_INVAL
@@ -44,8 +52,8 @@ def test_a_bad_cache_is_refused_by_every_operator(B, bad):
 
 
 def test_bad_arguments_of_write_are_refused(B):
-    L, kv, h, r = B.lib(), _kv(B), B.Heads(4 << 20, 128, 64), C.byref
-    odd, none = B.Heads((4 << 20) + 1, 128, 64), B.Heads(0, 128, 64)
+    L, kv, h, r = B.lib(), _kv(B), _heads(4 << 20, 128, 64), C.byref
+    odd, none = _heads((4 << 20) + 1, 128, 64), _heads(0, 128, 64)
     rope = B.RopeDesc(1 << 20, 64, 0, 1.0)
 
     def call(kv_=None, n=1, rows=0, pos=1 << 20, rope_=None, k=r(h), v=r(h), Hq=4, q=r(h), q_out=r(h)):
@@ -65,7 +73,7 @@ def test_bad_arguments_of_write_are_refused(B):
 
 
 def test_bad_arguments_of_attend_and_read_are_refused(B):
-    L, kv, h, r = B.lib(), _kv(B), B.Heads(4 << 20, 128, 64), C.byref
+    L, kv, h, r = B.lib(), _kv(B), _heads(4 << 20, 128, 64), C.byref
     need = L.psmc_paged_attend_scratch_bytes(2, 4, 2, 64)
 
     def attend(lens=1 << 20, extra=0, Hq=4, q=r(h), out=r(h), scratch=1 << 20, nbytes=need):
@@ -84,7 +92,7 @@ def test_bad_arguments_of_attend_and_read_are_refused(B):
 
 
 def test_the_context_forms_refuse_without_a_context(B):
-    L, h, r = B.lib(), B.Heads(4 << 20, 128, 64), C.byref
+    L, h, r = B.lib(), _heads(4 << 20, 128, 64), C.byref
     assert L.psmc_kv_paged_write(None, None, 0, 1, 0, 0, None, r(h), r(h), 0, None, None, 0) == B.E_INVAL
     assert L.psmc_kv_paged_attend(None, None, 0, 4, r(h), r(h), 1.0, 0, 1 << 20, 1 << 40, 0) == B.E_INVAL
     assert L.psmc_kv_paged_read(None, None, 0, 1 << 20, 1 << 20, 16, 2048, 1024, 0) == B.E_INVAL
