@@ -8,11 +8,11 @@
 //   plan    per tile of 32 rows: the sets of rows that hold the same block at block index j, and the runs of j over which
 //           a set stays the same: the tile's SEGMENTS.  A segment's queries (rows x query heads per key-value head) meet
 //           its keys and values together.
-//   attend  the work of all (tile, key-value head, segment, query tile) items is laid on one line, in steps of 64
+//   attend  the work of all (tile, key-value head, segment, query tile) items is laid on one line, in steps of 64 or 128
 //           positions, and cut into equal shares, one per CTA of a grid that fills the GPU: long rows are split, short
-//           ones are strung together, and no CTA waits for another.  The four warps of a CTA stream a step's keys and
-//           values through a ring of shared-memory stages (cp.async, 16 bytes per lane, the next items' steps among
-//           them) and divide it by queries, 16 to a warp, and where that leaves warps over, by positions.
+//           ones are strung together, and no CTA waits for another.  One warp of a CTA walks its share and has a ring of
+//           shared-memory stages filled with the steps' keys and values; four warps divide a step by queries, 16 to a
+//           warp, and where that leaves warps over, by positions.
 //   join    per (row, query head): the partial results of the row's segments and of the shares that split them.
 //
 // Scores and outputs are formed transposed, S^T = K Q^T and O^T = V^T P^T, on the warp-level matrix instructions: the 16
@@ -276,12 +276,15 @@ __device__ __forceinline__ int steps_before(int64_t bound, int64_t a, int w, int
 }
 
 // What the arithmetic of an item has to know of it; the copying side, which is ahead, leaves it in a queue.
-struct alignas(16) Item {
-    uint32_t mask;
+struct ItemHead {
     int tile, head, qt;
-    int nq, steps, p0;   // queries of this query tile; steps that are this worker's; the position at which they begin
+    int nq, steps;       // queries of this query tile; steps that are this worker's
     int alone;           // the whole of its rows, in this share
     int64_t slot;        // where the partial result of its query 0 goes
+};
+struct alignas(16) Item {
+    ItemHead head_part;
+    uint8_t rows[kTileRows];  // the segment's rows within the tile, in order
 };
 
 // One worker's walk along the line.  All threads of the CTA hold the same values.
@@ -409,15 +412,13 @@ struct Walk {
         enter_item(l, lo);
         if (s >= s_end) next_item(l);
     }
-    __device__ __forceinline__ Item item(const Line& l, int worker) const {
-        Item it;
-        it.mask = mask;
+    __device__ __forceinline__ ItemHead item(const Line& l, int worker) const {
+        ItemHead it;
         it.tile = tile;
         it.head = head;
         it.qt = qt;
         it.nq = nq;
         it.steps = s_end - s;
-        it.p0 = p0 + s * S::kStep;
         it.alone = s_first == 0 && s_end == steps && (whole & mask) == mask;
         it.slot = s_first > 0 ? l.first_rest + (int64_t)worker * (kGroups * S::kGroup)
                               : ((int64_t)tile * l.ls.H + head) * (kTileRows * kRowSegs * l.ls.ratio) + (int64_t)before * l.ls.ratio +
@@ -436,6 +437,13 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// the barrier counts this thread's arrival when its copies so far have landed
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void copies_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -485,11 +493,12 @@ __device__ __forceinline__ uint32_t codes_to_f16(uint32_t x) {
 }
 
 // Shape of a CTA's work.  DP: head_dim rounded up to what the tiles are unrolled for.
-// A stage holds the keys of a step, then its values: panels of 128 bytes of every position's row, a row's 16-byte units
-// exchanged among themselves by the row's number (unit u of row r lies at u ^ (r % 8)), so that the 8 rows an operand load
-// touches lie in different banks.  That is what tiled bulk copies write with 128-byte swizzling.
-constexpr int kWarps = 4;
-constexpr int kPanel = 128;
+// A stage holds the keys of a step, then its values: per slice of 16 positions, panels of 128 bytes of every row, a row's
+// 16-byte units exchanged among themselves by the row's number (unit u of row r lies at u ^ (r % 8)), so that the 8 rows an
+// operand load touches lie in different banks.  That is what tiled bulk copies write with 128-byte swizzling.
+constexpr int kWarps = 4;                      // of the arithmetic; two more copy
+constexpr int kThreads = (kWarps + 2) * 32;
+constexpr int kPanel = 128, kPanelOfSlice = 16 * kPanel;
 template <int DT_, int DP_>
 struct Shape {
     static constexpr int DT = DT_, DP = DP_;
@@ -497,6 +506,7 @@ struct Shape {
     static constexpr int kPanels = (DP * kElem + kPanel - 1) / kPanel;
     static constexpr int kStep = DT == PSMC_F32 && DP > 128 ? 32 : (DT == PSMC_F8 && DP <= 128 ? 128 : 64);  // positions
     static constexpr int kSlices = kStep / 16;                            // the 16 positions of an operand tile
+    static constexpr int kSlice = kPanelOfSlice * kPanels;                // bytes of one, of keys or values
     static constexpr int kPair = kSlices > kWarps ? 2 : 1;                // slices that a warp takes at a time
     static constexpr int kHalf = kStep * kPanel * kPanels;                // keys, then values
     static constexpr int kScales = DT == PSMC_F8 ? kStep : 0;             // scale bytes
@@ -506,193 +516,232 @@ struct Shape {
     static constexpr int kExtra = DT == PSMC_F32 ? kWarps * (8 * DP + 16 * 8) * 4 : 0;
     // shared memory of one CTA: half of an SM's 228 KB, or the 227 KB that one may have, less 1 KB that the system keeps of
     // each, 1 KB for the ring's alignment and what lies beside the ring
-    static constexpr int kBeside = 2100, kHalfSm = 114 * 1024 - 2048 - kBeside, kWholeSm = 227 * 1024 - 1024 - kBeside;
-    static constexpr int kCtas = 3 * kStage + kExtra <= kHalfSm ? 2 : 1;  // per SM
+    static constexpr int kBeside = 3200, kHalfSm = 114 * 1024 - 2048 - kBeside, kWholeSm = 227 * 1024 - 1024 - kBeside;
+    static constexpr int kCtas = DP <= 128 && 3 * kStage + kExtra <= kHalfSm ? 2 : 1;  // per SM (large heads need the registers)
     static constexpr int kFit = ((kCtas == 2 ? kHalfSm : kWholeSm) - kExtra) / kStage;
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
     static constexpr int kBytes = kStages * kStage + kExtra + 1024;
-    static_assert(kStages >= (DT == PSMC_F8 ? 3 : 2) && kStage >= kWarps * 8 * (DP + 4) * 4, "a ring; a stage holds the warps' outputs of a query tile");
+    static_assert(kStages >= 2 && kStage >= kWarps * 8 * (DP + 4) * 4, "a ring; a stage holds the warps' outputs of a query tile");
 };
 
 struct AttendArgs {
-    CUtensorMap k_map, v_map;  // pools as [block][head, position][component], for tiled copies
+    CUtensorMap map[2];  // pools of keys and values as [block][panel][head, position][component], for tiled copies
     PagedView c;
     PagedAttend a;
     Line l;
     FastDiv by_block, by_ratio;
     int q_words;         // queries start on 4-byte boundaries throughout
+    int one_copy;        // heads are whole panels: a tiled copy brings all panels of a slice
 };
 
 __device__ __forceinline__ void tiled_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(0), "r"(z), "r"(smem_u32(bar))
                  : "memory");
 }
 
-// The copying side of a walk.  Warp w copies a quarter of a step's positions; what a copy needs from the block table is
-// asked for two steps before it is issued.  Items are put into the queue when their first step is asked for, so they are
-// there, with a barrier in between, before their first step is worked on; the queue is longer than this side is ahead.
-//
-// TILED: blocks are multiples of 16 positions, so 16 positions of one head lie in one block and travel as one tiled bulk copy
-// per panel (and a 16-byte one for their scales): a few instructions per step, where 16 bytes per lane and copy took the
-// load path 700 to 2000 cycles of each step.  Other block lengths are copied that way, a position wherever it lies.
 constexpr int kQueue = 16;
+constexpr uint32_t kEnd = 0xffffffffu;
 
 template <class S>
 struct Shared {          // beside the ring
-    uint64_t full[S::kStages];           // TILED: a stage's copies have landed
-    uint32_t valid[S::kStages][S::kSlices];  // which of a slice's 16 positions hold something
-    int entries[4][S::kSlices];          // TILED: table entries of the steps asked for
+    uint64_t full[S::kStages], empty[S::kStages];
+    uint32_t valid[S::kStages][S::kSlices];  // which of a slice's 16 positions hold something; kEnd in the first: no more steps
+    int entries[2][4][S::kSlices];       // table entries of the steps asked for, of either copying warp
+    int opened;                          // items in the queue so far
     Item queue[kQueue];
-    uint8_t rows[2][kWarps][kTileRows];  // row lists of this item and the next
-    float2 stats[kWarps][16];            // {reference, sum} of each warp's queries
+    float2 stats[2][kWarps][16];         // {reference, sum} of each warp's queries, of this item and the one before
     float scaled[kWarps][16];            // its sum as a share of the largest reference of the query's slices
 };
 
-struct Pipe {            // the ring of stages as a CTA sees it
-    char* ring;
-    uint32_t ring_at;
-    int stage;           // the stage of the next step to be worked on
-    uint32_t phase;      // TILED: its barrier's
-    int worker, warp, lane;
-};
-
+// The warps that walk the share and copy, one the keys, one the values.  TILED: blocks are multiples of 16 positions, so 16
+// positions of one head lie in one block and travel as one tiled bulk copy (or, where a head is no whole number of panels,
+// one per panel).  Other block lengths are copied 16 bytes per lane, a position wherever it lies.  A tiled copy takes the
+// warp that issues it some 80 cycles, which is why the warps of the arithmetic do not, and why there are two of these.
+// What a step needs from the block table is asked for two steps before its copies are issued, by an asynchronous copy (a
+// load's result would be waited for as soon as it is passed on in a register).  Items are put into the queue when their
+// first step is asked for; the queue is longer than this warp can be ahead.
 template <class S, bool TILED>
 struct Feeder {
-    static constexpr int kMine = S::kStep / kWarps;     // positions per warp
-    static constexpr int kUnits = TILED ? (kMine + 15) / 16 : kMine;  // what a lane asks for: a slice, or a position
-    static constexpr int kSpan = TILED ? 16 : 1;
+    // whether a stage's barrier also counts every lane of a copying warp, for copies that are not bulk copies
+    static constexpr bool kLaneArrivals = !TILED || S::DT == PSMC_F8;
     struct Asked {
-        int entry;       // lane u: table entry of the warp's unit u (TILED: of the step in the ring of entries)
-        int in_block;    // lane u: head * block_len + offset in the block
+        int in_block;    // lane u: head * block_len + offset in the block, of slice u
         int live;        // lane u: positions of it that lie in the segment
+        int tile, head, row, p, p1;  // not TILED: the step itself
         bool any;        // whether there is a step at all
     };
     Walk<S> walk;
     Asked first, second;
     int items;           // put into the queue so far
     int asked;           // steps asked for so far
-    int scales, scales_at;  // not TILED, 8-bit: scale bytes on their way to a stage
+    int worker, lane;
+    int which;           // 0: keys, 1: values
 
-    // TILED: the slice a lane sees to; steps of 32 have two, and the even warps copy one each
-    static __device__ __forceinline__ int slice_of(const Pipe& pp) { return S::kSlices >= kWarps ? pp.warp * kUnits + pp.lane : pp.warp / 2; }
-    __device__ __forceinline__ Asked ask(const AttendArgs& g, const Pipe& pp, Shared<S>& sh) {
-        Asked q{-1, 0, 0, !walk.done};
-        if (walk.done) {
-            if (TILED) copies_commit();
-            ++asked;
-            return q;
+    __device__ __forceinline__ void open_item(const AttendArgs& g, Shared<S>& sh) {
+        Item& it = sh.queue[items % kQueue];
+        if (lane == 0) it.head_part = walk.item(g.l, worker);
+        if (walk.mask >> lane & 1) it.rows[__popc(walk.mask & ((1u << lane) - 1))] = (uint8_t)lane;
+        __syncwarp();
+        ++items;
+        if (lane == 0) {
+            __threadfence_block();
+            *const_cast<volatile int*>(&sh.opened) = items;
         }
-        if (walk.s == walk.s_first) {
-            if (pp.warp == 0 && pp.lane == 0) sh.queue[items % kQueue] = walk.item(g.l, pp.worker);
-            ++items;
+        // the queries will be loaded by the warps that need them; brought near by now, they cost them little
+        const int lines = (g.c.D * (S::DT == PSMC_F32 ? 4 : 2) + 127) / 128;
+        for (int x = lane; x < walk.nq * lines; x += 32) {
+            const int in_tile = x / lines, qi = walk.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
+            const int64_t row = walk.tile * kTileRows + it.rows[rank], qh = walk.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
+            const char* at = static_cast<const char*>(g.a.q.data) + (row * g.a.q.stride_row + qh * g.a.q.stride_head) * (S::DT == PSMC_F32 ? 4 : 2);
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(at + (x - in_tile * lines) * 128));
         }
-        const int p = walk.p0 + walk.s * S::kStep + pp.warp * kMine + pp.lane * kSpan;
-        if (pp.lane < kUnits && p < walk.p1 && (S::kSlices >= kWarps || !TILED || pp.warp % 2 == 0)) {
-            const int j = div_by(p, g.by_block), row = walk.tile * kTileRows + __ffs(walk.mask) - 1;
-            const int32_t* from = g.c.table + (int64_t)row * g.c.table_ld + j;
-            q.in_block = walk.head * g.c.block_len + (p - j * g.c.block_len);
-            q.live = min(kSpan, walk.p1 - p);
-            // an asynchronous copy, where a load's result would be waited for as soon as it is passed on in a register
-            if (TILED) copy4(smem_of(&sh.entries[asked % 4][slice_of(pp)]), from);
-            else q.entry = __ldg(from);
+    }
+    __device__ __forceinline__ Asked ask(const AttendArgs& g, Shared<S>& sh) {
+        Asked q{};
+        q.any = !walk.done;
+        if (!walk.done) {
+            if (walk.s == walk.s_first && which == 0) open_item(g, sh);
+            const int p = walk.p0 + walk.s * S::kStep, row = walk.tile * kTileRows + __ffs(walk.mask) - 1;
+            if (TILED) {
+                const int mine = p + lane * 16;
+                if (lane < S::kSlices && mine < walk.p1) {
+                    const int j = div_by(mine, g.by_block);
+                    q.in_block = walk.head * g.c.block_len + (mine - j * g.c.block_len);
+                    q.live = min(16, walk.p1 - mine);
+                    copy4(smem_of(&sh.entries[which][asked % 4][lane]), g.c.table + (int64_t)row * g.c.table_ld + j);
+                }
+            } else {
+                q.row = row;
+                q.head = walk.head;
+                q.p = p;
+                q.p1 = walk.p1;
+            }
+            if (++walk.s >= walk.s_end) walk.next_item(g.l);
         }
         if (TILED) copies_commit();
         ++asked;
-        if (++walk.s >= walk.s_end) walk.next_item(g.l);
         return q;
     }
     // copies of the step asked for first, into stage `to`
-    __device__ __forceinline__ void issue(const AttendArgs& g, int to, const Pipe& pp, Shared<S>& sh) {
-        const uint32_t stage = pp.ring_at + to * S::kStage;
-        const int warp = pp.warp, lane = pp.lane;
-        if (!TILED && S::DT == PSMC_F8) put_scales(pp);
-        if (first.any) {
-            if (TILED) {
-                copies_wait<1>();  // the entries asked for last may still be on their way
-                if (first.live > 0) first.entry = sh.entries[(asked - 2) % 4][slice_of(pp)];
-            }
-            const bool named = first.live > 0 && first.entry >= 0 && first.entry < g.c.n_blocks;
+    __device__ __forceinline__ void issue(const AttendArgs& g, int to, char* ring, Shared<S>& sh) {
+        char* stage = ring + to * S::kStage + which * S::kHalf;
+        uint8_t* scales = reinterpret_cast<uint8_t*>(ring) + to * S::kStage + 2 * S::kHalf + which * S::kScales;
+        const char* pool = which ? g.c.v : g.c.k;
+        if (TILED) {
+            copies_wait<1>();  // the entries asked for last may still be on their way
+            const int entry = first.live > 0 ? sh.entries[which][(asked - 2) % 4][lane] : -1;
+            const bool named = entry >= 0 && entry < g.c.n_blocks;
             if (first.live > 0 && !named) raise_status(g.a.status, PSMC_E_STATE);
-            if (TILED) {
-                const int slice = slice_of(pp);
-                const bool owner = lane < kUnits && (S::kSlices >= kWarps || warp % 2 == 0);
-                if (owner) sh.valid[to][slice] = named ? (1u << first.live) - 1u : 0u;
-                const int copies = __popc(__ballot_sync(kFull, owner && named));
-                if (lane == 0) mbar_expect_tx(&sh.full[to], copies * (2 * S::kPanels * 16 * kPanel + (S::DT == PSMC_F8 ? 32 : 0)));
-                __syncwarp();
-                if (owner && named) {
-                    const uint32_t dst = stage + slice * 16 * kPanel;
+            if (which == 0 && lane < S::kSlices) sh.valid[to][lane] = named ? (1u << first.live) - 1u : 0u;
+            const int copies = __popc(__ballot_sync(kFull, named));
+            __syncwarp();  // the masks are written before the barrier is arrived at
+            if (lane == 0) mbar_expect_tx(&sh.full[to], copies * S::kSlice);
+            __syncwarp();
+            if (named) {
+                const uint32_t dst = smem_of(stage) + lane * S::kSlice;
+                if (g.one_copy) {
+                    tiled_load(dst, &g.map[which], 0, first.in_block, entry, &sh.full[to]);
+                } else {
 #pragma unroll
-                    for (int x = 0; x < S::kPanels; ++x) {
-                        tiled_load(dst + x * (S::kStep * kPanel), &g.k_map, x * (kPanel / S::kElem), first.in_block, first.entry, &sh.full[to]);
-                        tiled_load(dst + S::kHalf + x * (S::kStep * kPanel), &g.v_map, x * (kPanel / S::kElem), first.in_block, first.entry, &sh.full[to]);
-                    }
-                    if (S::DT == PSMC_F8) {
-                        const int64_t off = (int64_t)first.entry * g.c.blk_bytes + g.c.scale_at + first.in_block;
-                        char* at = pp.ring + to * S::kStage + 2 * S::kHalf + slice * 16;
-                        bulk_load(at, g.c.k + off, 16, &sh.full[to]);
-                        bulk_load(at + S::kScales, g.c.v + off, 16, &sh.full[to]);
+                    for (int x = 0; x < S::kPanels; ++x)
+                        tiled_load(dst + x * kPanelOfSlice, &g.map[which], x * (kPanel / S::kElem), first.in_block, entry, &sh.full[to]);
+                }
+                if (S::DT == PSMC_F8) copy16(smem_of(scales + lane * 16), pool + (int64_t)entry * g.c.blk_bytes + g.c.scale_at + first.in_block, 16);
+            }
+            if (S::DT == PSMC_F8) copies_arrive(&sh.full[to]);
+        } else {
+            constexpr int kPerRow = S::kPanels * (kPanel / 16);
+            const int per_row = g.c.D * S::kElem / 16;
+#pragma unroll 1
+            for (int base = 0; base < S::kStep; base += 32) {
+                const int p = first.p + base + lane;
+                int64_t off = 0;
+                bool named = false;
+                if (p < first.p1) {
+                    const int j = div_by(p, g.by_block), entry = __ldg(g.c.table + (int64_t)first.row * g.c.table_ld + j);
+                    const int64_t in_block = first.head * g.c.block_len + (p - j * g.c.block_len);
+                    named = entry >= 0 && entry < g.c.n_blocks;
+                    if (!named) {
+                        raise_status(g.a.status, PSMC_E_STATE);
+                    } else {
+                        off = (int64_t)entry * g.c.blk_bytes + in_block * (g.c.D * S::kElem);
+                        if (S::DT == PSMC_F8)
+                            scales[base + lane] = __ldg(reinterpret_cast<const uint8_t*>(pool) + (int64_t)entry * g.c.blk_bytes + g.c.scale_at + in_block);
                     }
                 }
-            } else {
                 const uint32_t valid = __ballot_sync(kFull, named);
-                if (kMine >= 16) {
-                    if (lane < kMine / 16) sh.valid[to][warp * (kMine / 16) + lane] = valid >> (lane * 16) & 0xffffu;
-                } else {  // half a slice: a byte of its mask
-                    if (lane == 0) reinterpret_cast<uint16_t*>(&sh.valid[to][warp / 2])[warp % 2] = (uint16_t)valid;
-                }
-                const int64_t off = named ? (int64_t)first.entry * g.c.blk_bytes + (int64_t)first.in_block * (g.c.D * S::kElem) : 0;
-                constexpr int kPerRow = S::kPanels * (kPanel / 16);
-                const int per_row = g.c.D * S::kElem / 16;
+                if (which == 0 && lane < 2) sh.valid[to][base / 16 + lane] = valid >> (lane * 16) & 0xffffu;
 #pragma unroll 4
-                for (int i = 0; i < kMine * kPerRow / 32; ++i) {  // whole rows of panels: what lies beyond the head becomes zero
-                    const int x = i * 32 + lane, r = x / kPerRow, col = x - r * kPerRow, row = warp * kMine + r;
+                for (int i = 0; i < kPerRow; ++i) {  // whole rows of panels: what lies beyond the head becomes zero
+                    const int x = i * 32 + lane, r = x / kPerRow, col = x - r * kPerRow, row = base + r;
                     const int64_t from = (int64_t)__shfl_sync(kFull, (long long)off, r) + col * 16;
                     const int bytes = (valid >> r & 1) && col < per_row ? 16 : 0;
-                    const uint32_t dst = stage + (col / 8) * (S::kStep * kPanel) + row * kPanel + ((col % 8 ^ (row & 7)) << 4);
-                    copy16(dst, g.c.k + (bytes ? from : 0), bytes);
-                    copy16(dst + S::kHalf, g.c.v + (bytes ? from : 0), bytes);
-                }
-                if (S::DT == PSMC_F8) {
-                    scales_at = to;
-                    scales = 127 | 127 << 8;
-                    if (named) {
-                        const int64_t at = (int64_t)first.entry * g.c.blk_bytes + g.c.scale_at + first.in_block;
-                        scales = (int)__ldg(reinterpret_cast<const uint8_t*>(g.c.k) + at) | (int)__ldg(reinterpret_cast<const uint8_t*>(g.c.v) + at) << 8;
-                    }
+                    copy16(smem_of(stage) + (row / 16) * S::kSlice + (col / 8) * kPanelOfSlice + (row % 16) * kPanel + ((col % 8 ^ (row & 7)) << 4),
+                           pool + (bytes ? from : 0), bytes);
                 }
             }
+            copies_arrive(&sh.full[to]);
+            __syncwarp();
+            if (lane == 0) mbar_expect_tx(&sh.full[to], 0);
         }
-        if (!TILED) copies_commit();
         first = second;
-        second = ask(g, pp, sh);
+        second = ask(g, sh);
     }
-    // the scale bytes asked for with the step before this one: there by now, and needed a step from now at the earliest
-    __device__ __forceinline__ void put_scales(const Pipe& pp) {
-        if (scales_at >= 0 && pp.lane < kMine) {
-            uint8_t* at = reinterpret_cast<uint8_t*>(pp.ring) + scales_at * S::kStage + 2 * S::kHalf + pp.warp * kMine + pp.lane;
-            at[0] = (uint8_t)scales;
-            at[S::kScales] = (uint8_t)(scales >> 8);
+    __device__ __forceinline__ void run(const AttendArgs& g, char* ring, Shared<S>& sh) {
+        lane = threadIdx.x & 31;
+        worker = blockIdx.x;
+        which = (threadIdx.x >> 5) - kWarps;
+        items = asked = 0;
+        walk.begin(g.l, worker, lane);
+        first = ask(g, sh);
+        second = ask(g, sh);
+        int stage = 0;
+        uint32_t phase = 1;  // (a barrier that nothing has happened to yet lets the phase before its first pass)
+        for (;;) {
+            if (!mbar_wait(&sh.empty[stage], phase)) {
+                if (lane == 0) raise_status(g.a.status, PSMC_E_TIMEOUT);
+                return;
+            }
+            if (!first.any) {
+                if (lane == 0) {
+                    if (which == 0) sh.valid[stage][0] = kEnd;
+                    mbar_expect_tx(&sh.full[stage], 0);
+                }
+                if (kLaneArrivals) copies_arrive(&sh.full[stage]);
+                return;
+            }
+            issue(g, stage, ring, sh);
+            if (++stage == S::kStages) {
+                stage = 0;
+                phase ^= 1u;
+            }
         }
-        scales_at = -1;
-    }
-    // the next step to be worked on has landed, and everyone is done with the one before it; false: the wait ran out
-    __device__ __forceinline__ bool wait(const Pipe& pp, Shared<S>& sh) {
-        bool ok = true;
-        if (TILED) ok = mbar_wait(&sh.full[pp.stage], pp.phase);
-        else copies_wait<S::kStages - 2>();
-        if (TILED) return __syncthreads_and(ok);
-        __syncthreads();
-        return true;
     }
 };
 
-// row (within the tile) of each place in a segment's mask
-__device__ __forceinline__ void list_rows(uint32_t mask, uint8_t* rows, int lane) {
-    if (mask >> lane & 1) rows[__popc(mask & ((1u << lane) - 1))] = (uint8_t)lane;
+struct Pipe {            // the ring of stages as a warp of the arithmetic sees it
+    char* ring;
+    int stage;           // the stage of the next step
+    uint32_t phase;      // its barrier's
+    int worker, warp, lane;
+};
+template <class S>
+__device__ __forceinline__ bool landed(const Pipe& pp, Shared<S>& sh) { return mbar_wait(&sh.full[pp.stage], pp.phase); }
+// this warp is done with a stage; whatever it wrote there itself is ordered before the copies that come next
+template <class S>
+__device__ __forceinline__ void release(Shared<S>& sh, int stage, int lane) {
     __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.empty[stage]);
 }
+template <class S>
+__device__ __forceinline__ void next_stage(Pipe& pp) {
+    if (++pp.stage == S::kStages) {
+        pp.stage = 0;
+        pp.phase ^= 1u;
+    }
+}
+__device__ __forceinline__ void sync_warps() { asm volatile("bar.sync 1, 128;" ::: "memory"); }  // the four warps of the arithmetic
 
 template <typename T>
 __device__ __forceinline__ void put4(T* p, const float4& x) {  // p need not be aligned beyond its type
@@ -713,23 +762,9 @@ struct Division {
     }
 };
 
-__device__ __forceinline__ void next_stage(Pipe& pp, int stages) {
-    if (++pp.stage == stages) {
-        pp.stage = 0;
-        pp.phase ^= 1u;
-    }
-}
-
-// A slice's mask as it is kept: 16 bits, or a byte in each half (copied by position in steps of 32).
-template <class S, bool TILED>
-__device__ __forceinline__ uint32_t slice_valid(const uint32_t* valid, int m) {
-    const uint32_t v = valid[m];
-    return !TILED && S::kStep / kWarps < 16 ? (v & 0xffu) | (v >> 16 & 0xffu) << 8 : v;
-}
-
 // row and query head of query `in_tile` of an item
 template <class S>
-__device__ __forceinline__ void place(const AttendArgs& g, const Item& it, const uint8_t* rows, int in_tile, int* row, int* qh) {
+__device__ __forceinline__ void place(const AttendArgs& g, const ItemHead& it, const uint8_t* rows, int in_tile, int* row, int* qh) {
     const int qi = it.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
     *row = it.tile * kTileRows + rows[rank];
     *qh = it.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
@@ -741,7 +776,7 @@ struct RawQueries {      // lane (gq, t) holds components of query gq of each ti
     uint32_t x[2][S::DP / 16][2];
 };
 template <class S>
-__device__ __forceinline__ void load_queries(const AttendArgs& g, const Item& it, const uint8_t* rows, RawQueries<S>& q, const Pipe& pp) {
+__device__ __forceinline__ void load_queries(const AttendArgs& g, const ItemHead& it, const uint8_t* rows, RawQueries<S>& q, const Pipe& pp) {
     const Division dv(it.nq, S::kGroup, S::kSlices, pp.warp);
     const int t = pp.lane & 3, gq = pp.lane >> 2, q0 = dv.group * S::kGroup;
 #pragma unroll
@@ -828,7 +863,7 @@ struct Tiles {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     uint32_t ka[4];
-                    load_tiles(ka, keys[m] + krow + (2 * ks / 8) * (S::kStep * kPanel) + ((2 * ks % 8 << 4) ^ kunit));
+                    load_tiles(ka, keys[m] + krow + (2 * ks / 8) * kPanelOfSlice + ((2 * ks % 8 << 4) ^ kunit));
 #pragma unroll
                     for (int j = 0; j < NT; ++j) mma<false>(ks & 1 ? s2[m][j] : s[m][j], ka, q.x[j][ks][0], q.x[j][ks][1]);
                 }
@@ -838,7 +873,7 @@ struct Tiles {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     uint32_t kc[4];
-                    load_tiles(kc, keys[m] + krow + (ks / 8) * (S::kStep * kPanel) + ((ks % 8 << 4) ^ kunit));
+                    load_tiles(kc, keys[m] + krow + (ks / 8) * kPanelOfSlice + ((ks % 8 << 4) ^ kunit));
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const uint32_t ka[4] = {codes_to_f16(kc[2 * u]), codes_to_f16(kc[2 * u + 1]), codes_to_f16(kc[2 * u] >> 16),
@@ -929,7 +964,7 @@ struct Tiles {
 #pragma unroll
                 for (int d = 0; d < kDt; ++d) {
                     uint32_t va[4];
-                    load_tiles_turned(va, vals[m] + vrow + (2 * d / 8) * (S::kStep * kPanel) + ((2 * d % 8 << 4) ^ vunit));
+                    load_tiles_turned(va, vals[m] + vrow + (2 * d / 8) * kPanelOfSlice + ((2 * d % 8 << 4) ^ vunit));
 #pragma unroll
                     for (int j = 0; j < NT; ++j) {
                         mma<false>(o[j][d], va, p[m][j][0][0], p[m][j][0][1]);
@@ -942,7 +977,7 @@ struct Tiles {
 #pragma unroll
                 for (int d = 0; d < kDt; d += 2) {  // 32 components: the even ones, then the odd ones
                     uint32_t vc[4], va[2][4];
-                    load_tiles_turned(vc, vals[m] + vrow + (d / 8) * (S::kStep * kPanel) + ((d % 8 << 4) ^ vunit));
+                    load_tiles_turned(vc, vals[m] + vrow + (d / 8) * kPanelOfSlice + ((d % 8 << 4) ^ vunit));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {  // bytes (pos 0, d), (pos 0, d + 1), (pos 1, d), (pos 1, d + 1)
                         const uint32_t x = __byte_perm(vc[e], 0, 0x3120);
@@ -970,7 +1005,7 @@ __device__ __forceinline__ void clear_rows(char* vals, uint32_t valid, int lane)
     for (uint32_t dead = ~valid & 0xffffu; dead; dead &= dead - 1) {
         const int r = __ffs(dead) - 1;
         for (int u = lane; u < S::kPanels * 8; u += 32)
-            *reinterpret_cast<uint4*>(vals + (u / 8) * (S::kStep * kPanel) + r * kPanel + (u % 8) * 16) = uint4{0, 0, 0, 0};
+            *reinterpret_cast<uint4*>(vals + (u / 8) * kPanelOfSlice + r * kPanel + (u % 8) * 16) = uint4{0, 0, 0, 0};
     }
     fence_async_smem();  // before a copy may write there again
     __syncwarp();
@@ -980,8 +1015,8 @@ __device__ __forceinline__ void clear_rows(char* vals, uint32_t valid, int lane)
 // slices: summed over the slices and written, to the queries' rows or as partial results, 16 bytes per lane.  first: the
 // tile's first query within a warp's group.
 template <class S>
-__device__ __forceinline__ void write_tile(const AttendArgs& g, const Item& it, const Division& dv, const float* carry, const Shared<S>& sh,
-                                           const uint8_t* rows, int first, const Pipe& pp) {
+__device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& it, const Division& dv, const float* carry, const Shared<S>& sh,
+                                           const uint8_t* rows, int first, const Pipe& pp, int index) {
     using T = typename PoolIo<S::DT>::type;
     constexpr int kPitch = S::DP + 4;
     for (int u = 0; u < 2 * dv.groups; ++u) {  // the warps share the queries evenly
@@ -991,7 +1026,7 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const Item& it, 
 #pragma unroll
         for (int z = 0; z < kWarps; ++z)
             if (z < dv.slices) {
-                top = fmaxf(top, sh.stats[z * dv.groups + grp][first + ql].x);
+                top = fmaxf(top, sh.stats[index & 1][z * dv.groups + grp][first + ql].x);
                 total += sh.scaled[z * dv.groups + grp][first + ql];
             }
         int row, qh;
@@ -1025,24 +1060,33 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const Item& it, 
     }
 }
 
-// One item, from its queries (already asked for) to its result.  NT: tiles of 8 queries per warp.
+// One item, from its queries to its result.  NT: tiles of 8 queries per warp.  has_q: the queries have been loaded already;
+// afterwards, whether the next item's have.  false: a wait ran out.
 template <class S, bool TILED, int NT>
-__device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, RawQueries<S>& q, Feeder<S, TILED>& feed, Pipe& pp, Shared<S>& sh,
-                                         int index) {
+__device__ __forceinline__ bool run_item(const AttendArgs& g, RawQueries<S>& q, bool& has_q, Pipe& pp, Shared<S>& sh, int index) {
     using Ti = Tiles<S, NT>;
     constexpr bool kF8 = S::DT == PSMC_F8;
     constexpr int kMost = NT == 1 || S::DP <= 128 ? S::kPair : 1;  // slices at a time
+    const ItemHead it = sh.queue[index % kQueue].head_part;
+    const uint8_t* rows = sh.queue[index % kQueue].rows;
     const int lane = pp.lane, warp = pp.warp, t = lane & 3, gq = lane >> 2;
     const Division dv(it.nq, S::kGroup, S::kSlices, warp);
     const bool busy = dv.slice < dv.slices && dv.group * S::kGroup < it.nq;
+    bool fine = true;
+    if (!has_q) load_queries<S>(g, it, rows, q, pp);
     Ti ti;
     ti.clear(q, g.a.scale * kLog2e, lane);
+    int used = pp.stage;  // the stage worked on last: kept until the result is written, which passes through it
 #pragma unroll 1
     for (int s = 0; s < it.steps; ++s) {
-        if (!feed.wait(pp, sh)) return false;
-        feed.issue(g, pp.stage == 0 ? S::kStages - 1 : pp.stage - 1, pp, sh);
+        if (s > 0) release<S>(sh, used, lane);
+        if (!landed<S>(pp, sh)) {
+            fine = false;
+            break;
+        }
+        used = pp.stage;
         if (busy) {
-            char* at = pp.ring + pp.stage * S::kStage;
+            char* at = pp.ring + used * S::kStage;
 #pragma unroll 1
             for (int m0 = dv.slice; m0 < S::kSlices; m0 += kMost * dv.slices) {
                 uint32_t keys[kMost], vals[kMost], valid[kMost];
@@ -1052,9 +1096,9 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, Ra
 #pragma unroll
                 for (int i = 0; i < kMost; ++i) {
                     const int m = m0 + i * dv.slices;
-                    keys[i] = smem_of(at) + m * 16 * kPanel;
+                    keys[i] = smem_of(at) + m * S::kSlice;
                     vals[i] = keys[i] + S::kHalf;
-                    valid[i] = slice_valid<S, TILED>(sh.valid[pp.stage], m);
+                    valid[i] = sh.valid[used][m];
                     any |= valid[i];
                     k_scale[i] = 1.f;
                     v_byte[i] = 127;
@@ -1068,18 +1112,19 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, Ra
                 if (TILED)
 #pragma unroll
                     for (int i = 0; i < kMost; ++i)
-                        if (valid[i] != 0xffffu) clear_rows<S>(at + S::kHalf + (m0 + i * dv.slices) * 16 * kPanel, valid[i], lane);
+                        if (valid[i] != 0xffffu) clear_rows<S>(at + S::kHalf + (m0 + i * dv.slices) * S::kSlice, valid[i], lane);
                 ti.template step<kMost>(q, keys, vals, valid, k_scale, v_byte, lane);
             }
         }
-        next_stage(pp, S::kStages);
+        next_stage<S>(pp);
     }
-    // ---- the next item's queries travel while this one's result is put together
-    if (index + 1 < feed.items) {
-        const Item next = sh.queue[(index + 1) % kQueue];
-        uint8_t* rows = sh.rows[(index + 1) & 1][warp];
-        list_rows(next.mask, rows, lane);
-        load_queries<S>(g, next, rows, q, pp);
+    // ---- the next item's queries travel while this one's result is put together, if the copying warp has got to it
+    has_q = false;
+    if (fine && *const_cast<volatile int*>(&sh.opened) > index + 1) {
+        __threadfence_block();
+        const Item& next = sh.queue[(index + 1) % kQueue];
+        load_queries<S>(g, next.head_part, next.rows, q, pp);
+        has_q = true;
     }
     // ---- sums over the lanes that hold parts of them, then over the slices
 #pragma unroll
@@ -1091,10 +1136,10 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, Ra
             x += __shfl_xor_sync(kFull, x, 8);
             x += __shfl_xor_sync(kFull, x, 16);
             ti.sum[j][i] = x;
-            if (gq == 0) sh.stats[warp][j * 8 + 2 * t + i] = float2{ti.ref[j][i], x};
+            if (gq == 0) sh.stats[index & 1][warp][j * 8 + 2 * t + i] = float2{ti.ref[j][i], x};
         }
-    __syncthreads();  // also: everyone is done with the last step's stage, which now carries the outputs
-    float* carry = reinterpret_cast<float*>(pp.ring + (pp.stage == 0 ? S::kStages - 1 : pp.stage - 1) * S::kStage);
+    sync_warps();  // also: everyone is done with the last step's stage, which now carries the outputs
+    float* carry = reinterpret_cast<float*>(pp.ring + used * S::kStage);
     constexpr int kPitch = S::DP + 4;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -1104,7 +1149,7 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, Ra
                 float top = -INFINITY;
 #pragma unroll
                 for (int z = 0; z < kWarps; ++z)
-                    if (z < dv.slices) top = fmaxf(top, sh.stats[z * dv.groups + dv.group][j * 8 + 2 * t + i].x);
+                    if (z < dv.slices) top = fmaxf(top, sh.stats[index & 1][z * dv.groups + dv.group][j * 8 + 2 * t + i].x);
                 // (a factor of zero keeps a NaN that came with the values)
                 const float f = ti.ref[j][i] == top ? 1.f : (ti.ref[j][i] == -INFINITY ? 0.f : ex2(ti.ref[j][i] - top));
                 if (gq == 0) sh.scaled[warp][j * 8 + 2 * t + i] = ti.sum[j][i] * f;
@@ -1114,76 +1159,66 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, const Item& it, Ra
                     for (int e = 0; e < 2; ++e)
                         carry[(warp * 8 + 2 * t + i) * kPitch + Ti::component(d, e, lane)] = ti.o[j][d][2 * e + i] * f;
             }
-        __syncthreads();
-        write_tile<S>(g, it, dv, carry, sh, sh.rows[index & 1][warp], j * 8, pp);
-        if (j + 1 < NT) __syncthreads();
+        sync_warps();
+        write_tile<S>(g, it, dv, carry, sh, rows, j * 8, pp, index);
+        if (j + 1 < NT) sync_warps();
     }
-    if (TILED) fence_async_smem();  // before a copy may write there again
-    return true;
+    if (TILED) fence_async_smem();
+    release<S>(sh, used, lane);
+    return fine;
 }
 
+// Sets the CTA up; true for the warps of the arithmetic.
 template <class S, bool TILED>
-__device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe& pp, Shared<S>& sh, Feeder<S, TILED>& feed) {
+__device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe& pp, Shared<S>& sh) {
     pp.ring = smem + (-(int)smem_of(smem) & 1023);
-    pp.ring_at = smem_of(pp.ring);
     pp.stage = 0;
     pp.phase = 0;
     pp.lane = threadIdx.x & 31;
     pp.warp = threadIdx.x >> 5;
     pp.worker = blockIdx.x;
-    if (TILED && threadIdx.x == 0) {
-        for (int i = 0; i < S::kStages; ++i) mbar_init(&sh.full[i], kWarps);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(&sh.full[i], 2 * (Feeder<S, TILED>::kLaneArrivals ? 33 : 1));
+            mbar_init(&sh.empty[i], kWarps);
+        }
+        sh.opened = 0;
         fence_async_smem();
     }
+    __syncthreads();
     chain_begin();
-    feed.walk.begin(g.l, pp.worker, pp.lane);
-    feed.items = feed.asked = 0;
-    feed.scales_at = -1;
-    if (feed.walk.done) return false;
-    feed.first = feed.ask(g, pp, sh);
-    feed.second = feed.ask(g, pp, sh);
-    __syncthreads();  // the barriers are ready, the first item is in the queue
-    return true;
-}
-template <class S, bool TILED>
-__device__ __forceinline__ void fill_pipe(const AttendArgs& g, Pipe& pp, Shared<S>& sh, Feeder<S, TILED>& feed) {
-#pragma unroll 1
-    for (int i = 0; i < S::kStages - 1; ++i) feed.issue(g, i, pp, sh);
+    if (pp.warp < kWarps) return true;
+    Feeder<S, TILED> feed;
+    feed.run(g, pp.ring, sh);
+    return false;
 }
 // A wait for a copy ran out: says so, and gives the copies that are still on their way their time before the CTA ends.
 template <class S>
-__device__ __forceinline__ void give_up(const AttendArgs& g, const Pipe& pp, Shared<S>& sh) {
-    if (threadIdx.x == 0) raise_status(g.a.status, PSMC_E_TIMEOUT);
-    int stage = pp.stage;
-    uint32_t phase = pp.phase;
+__device__ __forceinline__ void give_up(const AttendArgs& g, Pipe pp, Shared<S>& sh) {
+    if (pp.lane == 0) raise_status(g.a.status, PSMC_E_TIMEOUT);
     for (int i = 0; i < S::kStages; ++i) {
-        mbar_wait(&sh.full[stage], phase);
-        if (++stage == S::kStages) {
-            stage = 0;
-            phase ^= 1u;
-        }
+        landed<S>(pp, sh);
+        next_stage<S>(pp);
     }
 }
 
 template <class S, bool TILED>
-__global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_kernel(const __grid_constant__ AttendArgs g) {
+__global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_kernel(const __grid_constant__ AttendArgs g) {
     extern __shared__ __align__(1024) char smem[];
     __shared__ Shared<S> sh;
     static_assert(sizeof(sh) <= S::kBeside, "beside the ring");
     Pipe pp;
-    Feeder<S, TILED> feed;
-    if (!open_pipe<S, TILED>(g, smem, pp, sh, feed)) return;
+    if (!open_pipe<S, TILED>(g, smem, pp, sh)) return;
     RawQueries<S> q;
-    {
-        const Item it = sh.queue[0];
-        list_rows(it.mask, sh.rows[0][pp.warp], pp.lane);
-        load_queries<S>(g, it, sh.rows[0][pp.warp], q, pp);
-    }
-    fill_pipe<S, TILED>(g, pp, sh, feed);
-    for (int index = 0; index < feed.items; ++index) {
-        const Item it = sh.queue[index % kQueue];
-        const bool ok = it.nq <= 8 ? run_item<S, TILED, 1>(g, it, q, feed, pp, sh, index) : run_item<S, TILED, 2>(g, it, q, feed, pp, sh, index);
-        if (!ok) {
+    bool has_q = false;
+    for (int index = 0;; ++index) {
+        bool fine = landed<S>(pp, sh);
+        if (fine) {
+            if (sh.valid[pp.stage][0] == kEnd) return;
+            fine = sh.queue[index % kQueue].head_part.nq <= 8 ? run_item<S, TILED, 1>(g, q, has_q, pp, sh, index)
+                                                              : run_item<S, TILED, 2>(g, q, has_q, pp, sh, index);
+        }
+        if (!fine) {
             give_up<S>(g, pp, sh);
             return;
         }
@@ -1194,14 +1229,15 @@ __global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_kernel(con
 // scores: a lane has one position, and four queries (NQ = 8) or half of the components of four (NQ = 4); in the second
 // product a lane owns DP / 32 components of all queries.
 template <class S, bool TILED, int NQ>
-__device__ __forceinline__ bool run_item_f32(const AttendArgs& g, const Item& it, float* qs, float* ps, Feeder<S, TILED>& feed, Pipe& pp,
-                                             Shared<S>& sh, int index) {
+__device__ __forceinline__ bool run_item_f32(const AttendArgs& g, float* qs, float* ps, Pipe& pp, Shared<S>& sh, int index) {
     constexpr int kOwn = S::DP / 32;
     static_assert(S::kPair == 1, "one slice at a time");
+    const ItemHead it = sh.queue[index % kQueue].head_part;
+    const uint8_t* rows = sh.queue[index % kQueue].rows;
     const int lane = pp.lane, warp = pp.warp, key = lane & 15, half = lane >> 4, qh4 = NQ == 8 ? half * 4 : 0;
     const Division dv(it.nq, S::kGroup, S::kSlices, warp);
     const int q0 = dv.group * S::kGroup, mine = dv.slice < dv.slices ? min(S::kGroup, it.nq - q0) : 0;  // may be <= 0
-    const uint8_t* rows = sh.rows[index & 1][warp];
+    bool fine = true;
     {
         float x[NQ][kOwn];
 #pragma unroll
@@ -1229,16 +1265,21 @@ __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, const Item& it
         sum[u] = 0.f;
     }
     __syncwarp();
+    int used = pp.stage;  // the stage worked on last: kept until the result is written, which passes through it
 #pragma unroll 1
     for (int st = 0; st < it.steps; ++st) {
-        if (!feed.wait(pp, sh)) return false;
-        feed.issue(g, pp.stage == 0 ? S::kStages - 1 : pp.stage - 1, pp, sh);
+        if (st > 0) release<S>(sh, used, lane);
+        if (!landed<S>(pp, sh)) {
+            fine = false;
+            break;
+        }
+        used = pp.stage;
 #pragma unroll 1
         for (int m = dv.slice; m < S::kSlices && mine > 0; m += dv.slices) {
-            const uint32_t has = slice_valid<S, TILED>(sh.valid[pp.stage], m);
+            const uint32_t has = sh.valid[used][m];
             if (has == 0) continue;
             const bool ok = has >> key & 1;
-            char* keys = pp.ring + pp.stage * S::kStage + m * 16 * kPanel;
+            char* keys = pp.ring + used * S::kStage + m * S::kSlice;
             if (TILED && has != 0xffffu) clear_rows<S>(keys + S::kHalf, has, lane);
             float s[4] = {0.f, 0.f, 0.f, 0.f};
             constexpr int kSpan = NQ == 8 ? S::DP : S::DP / 2;
@@ -1246,7 +1287,7 @@ __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, const Item& it
 #pragma unroll 8
             for (int d = 0; d < kSpan; d += 4) {
                 const int u4 = (d0 + d) / 4;  // unit of the row
-                const float4 k = *reinterpret_cast<const float4*>(keys + (u4 / 8) * (S::kStep * kPanel) + key * kPanel + ((u4 % 8 ^ (key & 7)) << 4));
+                const float4 k = *reinterpret_cast<const float4*>(keys + (u4 / 8) * kPanelOfSlice + key * kPanel + ((u4 % 8 ^ (key & 7)) << 4));
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const float4 q = *reinterpret_cast<const float4*>(qs + (qh4 + u) * S::DP + d0 + d);
@@ -1293,58 +1334,58 @@ __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, const Item& it
                 }
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i) {
-                    const float v = *reinterpret_cast<const float*>(vals + i * (S::kStep * kPanel) + p * kPanel + ((lane >> 2 ^ (p & 7)) << 4) + (lane & 3) * 4);
+                    const float v = *reinterpret_cast<const float*>(vals + i * kPanelOfSlice + p * kPanel + ((lane >> 2 ^ (p & 7)) << 4) + (lane & 3) * 4);
 #pragma unroll
                     for (int j = 0; j < NQ; ++j) o[j][i] = fmaf(w[j], v, o[j][i]);
                 }
             }
             __syncwarp();
         }
-        next_stage(pp, S::kStages);
+        next_stage<S>(pp);
     }
-    if (index + 1 < feed.items) list_rows(sh.queue[(index + 1) % kQueue].mask, sh.rows[(index + 1) & 1][warp], lane);
     // ---- sums over the lanes, then over the slices
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
 #pragma unroll
         for (int x = 1; x < 16; x <<= 1) sum[u] += __shfl_xor_sync(kFull, sum[u], x);
-        if (key == 0 && (NQ == 8 || half == 0)) sh.stats[warp][qh4 + u] = float2{ref[u], sum[u]};
+        if (key == 0 && (NQ == 8 || half == 0)) sh.stats[index & 1][warp][qh4 + u] = float2{ref[u], sum[u]};
     }
-    __syncthreads();  // also: everyone is done with the last step's stage, which now carries the outputs
-    float* carry = reinterpret_cast<float*>(pp.ring + (pp.stage == 0 ? S::kStages - 1 : pp.stage - 1) * S::kStage);
+    sync_warps();  // also: everyone is done with the last step's stage, which now carries the outputs
+    float* carry = reinterpret_cast<float*>(pp.ring + used * S::kStage);
     if (mine > 0)
 #pragma unroll
         for (int j = 0; j < NQ; ++j) {
             float top = -INFINITY;
-            for (int z = 0; z < dv.slices; ++z) top = fmaxf(top, sh.stats[z * dv.groups + dv.group][j].x);
-            const float own = sh.stats[warp][j].x, f = own == top ? 1.f : (own == -INFINITY ? 0.f : exp2f(own - top));
-            if (lane == 0) sh.scaled[warp][j] = sh.stats[warp][j].y * f;
+            for (int z = 0; z < dv.slices; ++z) top = fmaxf(top, sh.stats[index & 1][z * dv.groups + dv.group][j].x);
+            const float own = sh.stats[index & 1][warp][j].x, f = own == top ? 1.f : (own == -INFINITY ? 0.f : exp2f(own - top));
+            if (lane == 0) sh.scaled[warp][j] = sh.stats[index & 1][warp][j].y * f;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) carry[(warp * 8 + j) * (S::DP + 4) + lane + 32 * i] = o[j][i] * f;
         }
-    __syncthreads();
-    write_tile<S>(g, it, dv, carry, sh, rows, 0, pp);
-    if (TILED) fence_async_smem();  // before a copy may write there again
-    return true;
+    sync_warps();
+    write_tile<S>(g, it, dv, carry, sh, rows, 0, pp, index);
+    if (TILED) fence_async_smem();
+    release<S>(sh, used, lane);
+    return fine;
 }
 
 template <class S, bool TILED>
-__global__ void __launch_bounds__(kWarps * 32, S::kCtas) paged_attend_f32_kernel(const __grid_constant__ AttendArgs g) {
+__global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_f32_kernel(const __grid_constant__ AttendArgs g) {
     extern __shared__ __align__(1024) char smem[];
     __shared__ Shared<S> sh;
     static_assert(sizeof(sh) <= S::kBeside, "beside the ring");
     Pipe pp;
-    Feeder<S, TILED> feed;
-    if (!open_pipe<S, TILED>(g, smem, pp, sh, feed)) return;
+    if (!open_pipe<S, TILED>(g, smem, pp, sh)) return;
     float* qs = reinterpret_cast<float*>(pp.ring + S::kStages * S::kStage) + pp.warp * (8 * S::DP + 16 * 8);  // [8][DP]
     float* ps = qs + 8 * S::DP;                                                                               // [16][8]
-    list_rows(sh.queue[0].mask, sh.rows[0][pp.warp], pp.lane);
-    fill_pipe<S, TILED>(g, pp, sh, feed);
-    for (int index = 0; index < feed.items; ++index) {
-        const Item it = sh.queue[index % kQueue];
-        const bool ok = it.nq <= 4 ? run_item_f32<S, TILED, 4>(g, it, qs, ps, feed, pp, sh, index)
-                                   : run_item_f32<S, TILED, 8>(g, it, qs, ps, feed, pp, sh, index);
-        if (!ok) {
+    for (int index = 0;; ++index) {
+        bool fine = landed<S>(pp, sh);
+        if (fine) {
+            if (sh.valid[pp.stage][0] == kEnd) return;
+            fine = sh.queue[index % kQueue].head_part.nq <= 4 ? run_item_f32<S, TILED, 4>(g, qs, ps, pp, sh, index)
+                                                              : run_item_f32<S, TILED, 8>(g, qs, ps, pp, sh, index);
+        }
+        if (!fine) {
             give_up<S>(g, pp, sh);
             return;
         }
@@ -1508,9 +1549,9 @@ Scratch scratch_of(int R, int Hq, int D) {
     return s;
 }
 
-// A pool as a tensor of three dimensions for tiled copies of 16 positions x 128 bytes, swizzled; components beyond the head
-// read as zero.
-bool tile_map(CUtensorMap* map, const PagedView& c, const char* pool) {
+// A pool as a tensor for tiled copies of 16 positions, swizzled: components of a panel, (head, position), panels, blocks; where a
+// head is no whole number of panels, all components, (head, position), 1, blocks (components beyond the head read as zero).
+bool tile_map(CUtensorMap* map, const PagedView& c, const char* pool, int panels) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static const Encode encode = [] {
@@ -1524,10 +1565,13 @@ bool tile_map(CUtensorMap* map, const PagedView& c, const char* pool) {
     const int elem = c.dt == PSMC_F32 ? 4 : (c.dt == PSMC_BF16 ? 2 : 1);
     const CUtensorMapDataType type = c.dt == PSMC_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                                       : (c.dt == PSMC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8);
-    const cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)c.H * c.block_len, (cuuint64_t)c.n_blocks};
-    const cuuint64_t strides[2] = {(cuuint64_t)c.D * elem, (cuuint64_t)c.blk_bytes};
-    const cuuint32_t box[3] = {(cuuint32_t)(kPanel / elem), 16, 1}, unit[3] = {1, 1, 1};
-    return encode(map, type, 3, const_cast<char*>(pool), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    // (a panel count below what the kernel is unrolled for is possible: the others lie outside and read as zero)
+    const bool whole = c.D * elem % kPanel == 0;
+    const cuuint64_t dims[4] = {(cuuint64_t)(whole ? kPanel / elem : c.D), (cuuint64_t)c.H * c.block_len, (cuuint64_t)(whole ? c.D * elem / kPanel : 1),
+                                (cuuint64_t)c.n_blocks};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.D * elem, (cuuint64_t)kPanel, (cuuint64_t)c.blk_bytes};
+    const cuuint32_t box[4] = {(cuuint32_t)(kPanel / elem), 16, (cuuint32_t)(whole ? panels : 1), 1}, unit[4] = {1, 1, 1, 1};
+    return encode(map, type, 4, const_cast<char*>(pool), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1553,12 +1597,13 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     cudaError_t e = launch_chained(paged_plan_kernel, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
     if (e != cudaSuccess) return e;
     const bool tiled = c.block_len % 16 == 0;
-    if (tiled && (!tile_map(&g.k_map, c, c.k) || !tile_map(&g.v_map, c, c.v))) return cudaErrorInvalidValue;
+    g.one_copy = c.D * S::kElem % kPanel == 0 ? 1 : 0;
+    if (tiled && (!tile_map(&g.map[0], c, c.k, S::kPanels) || !tile_map(&g.map[1], c, c.v, S::kPanels))) return cudaErrorInvalidValue;
     void (*fn)(const AttendArgs);
     if constexpr (DT == PSMC_F32) fn = tiled ? paged_attend_f32_kernel<S, true> : paged_attend_f32_kernel<S, false>;
     else fn = tiled ? paged_attend_kernel<S, true> : paged_attend_kernel<S, false>;
     e = allow_dynamic_smem(reinterpret_cast<const void*>(fn), S::kBytes);
-    if (e == cudaSuccess) e = launch_chained(fn, dim3((unsigned)g.l.workers), dim3(kWarps * 32), S::kBytes, stream, g);
+    if (e == cudaSuccess) e = launch_chained(fn, dim3((unsigned)g.l.workers), dim3(kThreads), S::kBytes, stream, g);
     if (e != cudaSuccess) return e;
     // few queries: four warps each, for what may be many partial results of a long row
     const int64_t queries = (int64_t)c.R * a.Hq;
