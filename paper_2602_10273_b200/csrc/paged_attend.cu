@@ -61,9 +61,11 @@ __device__ __forceinline__ int step_cost(int group, int nq) {
     const int groups = (nq + group - 1) / group;
     return 4 + (groups > 1 ? groups : 0);
 }
+// and an item beside its steps, for putting its result together
+constexpr int kItemCost = 5;
 __device__ __forceinline__ int64_t seg_cost(const LineShape& s, int rows, int steps) {
     const int nq = rows * s.ratio, qt = s.group * kGroups, full = nq / qt, rem = nq - full * qt;
-    return (int64_t)steps * (full * step_cost(s.group, qt) + (rem ? step_cost(s.group, rem) : 0));
+    return (int64_t)steps * (full * step_cost(s.group, qt) + (rem ? step_cost(s.group, rem) : 0)) + (full + (rem > 0)) * kItemCost;
 }
 __device__ __forceinline__ int steps_of(const LineShape& s, int p0, int p1) { return (p1 - p0 + s.step - 1) / s.step; }
 
@@ -248,7 +250,7 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
     Bearings b;
     b.total = sum;
     b.share = quotient(b.total + l.workers - 1, l.workers);
-    if (b.share < 4) b.share = 4;  // one step
+    if (b.share < 4 + kItemCost) b.share = 4 + kItemCost;  // an item of one step
     const int64_t x = worker * b.share;
     int64_t base = 0;
     b.tile = l.n_tiles;
@@ -270,8 +272,8 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
 }
 // the steps of an item (first cost unit a, cost w per step) that lie before `bound`
 __device__ __forceinline__ int steps_before(int64_t bound, int64_t a, int w, int steps) {
-    if (bound <= a) return 0;
-    const int64_t d = bound - a;
+    const int64_t d = bound - a - kItemCost;
+    if (d <= 0) return 0;
     return d >= (int64_t)steps * w ? steps : (int)(((uint32_t)d + (uint32_t)w - 1) / (uint32_t)w);
 }
 
@@ -331,7 +333,7 @@ struct Walk {
     // the item after this one that has a step for this worker
     __device__ __forceinline__ void next_item(const Line& l) {
         do {
-            a += (int64_t)steps * w;
+            a += (int64_t)steps * w + kItemCost;
             if (a >= hi) {
                 done = true;
                 return;
@@ -406,7 +408,7 @@ struct Walk {
             start = tp.seg[s0 + lane].start;
         }
         enter_segment(l, g);
-        const int64_t full = (int64_t)steps * step_cost(S::kGroup, kGroups * S::kGroup);
+        const int64_t full = (int64_t)steps * step_cost(S::kGroup, kGroups * S::kGroup) + kItemCost;
         qt = (int)min((int64_t)(n_qt - 1), quotient(y - first, full));
         a = b.before + head * cost + first + qt * full;
         enter_item(l, lo);
@@ -520,7 +522,12 @@ struct Shape {
     static constexpr int kCtas = DP <= 128 && 3 * kStage + kExtra <= kHalfSm ? 2 : 1;  // per SM (large heads need the registers)
     static constexpr int kFit = ((kCtas == 2 ? kHalfSm : kWholeSm) - kExtra) / kStage;
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
-    static constexpr int kBytes = kStages * kStage + kExtra + 1024;
+    // a step's stage has a slot for the queries of an item that begins with it: as many as there is room for, 8 or 16
+    static constexpr int kQueryRow = DP * 2 + 16;
+    static constexpr int kLeft = (kCtas == 2 ? kHalfSm : kWholeSm) - kExtra - kStages * kStage;
+    static constexpr int kSlotQueries = DT == PSMC_F32 ? 0 : (kLeft >= kStages * 16 * kQueryRow ? 16 : (kLeft >= kStages * 8 * kQueryRow ? 8 : 0));
+    static constexpr int kSlots = kSlotQueries * kQueryRow;  // bytes per stage
+    static constexpr int kBytes = kStages * (kStage + kSlots) + kExtra + 1024;
     static_assert(kStages >= 2 && kStage >= kWarps * 8 * (DP + 4) * 4, "a ring; a stage holds the warps' outputs of a query tile");
 };
 
@@ -529,8 +536,8 @@ struct AttendArgs {
     PagedView c;
     PagedAttend a;
     Line l;
-    FastDiv by_block, by_ratio;
-    int q_words;         // queries start on 4-byte boundaries throughout
+    FastDiv by_block, by_ratio, by_units;
+    int q_words, q_units;  // queries start on 4-byte, 16-byte boundaries throughout
     int one_copy;        // heads are whole panels: a tiled copy brings all panels of a slice
 };
 
@@ -548,11 +555,18 @@ struct Shared {          // beside the ring
     uint64_t full[S::kStages], empty[S::kStages];
     uint32_t valid[S::kStages][S::kSlices];  // which of a slice's 16 positions hold something; kEnd in the first: no more steps
     int entries[2][4][S::kSlices];       // table entries of the steps asked for, of either copying warp
-    int opened;                          // items in the queue so far
     Item queue[kQueue];
     float2 stats[2][kWarps][16];         // {reference, sum} of each warp's queries, of this item and the one before
     float scaled[kWarps][16];            // its sum as a share of the largest reference of the query's slices
 };
+
+// row and query head of query `in_tile` of an item
+template <class S>
+__device__ __forceinline__ void place(const AttendArgs& g, const ItemHead& it, const uint8_t* rows, int in_tile, int* row, int* qh) {
+    const int qi = it.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
+    *row = it.tile * kTileRows + rows[rank];
+    *qh = it.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
+}
 
 // The warps that walk the share and copy, one the keys, one the values.  TILED: blocks are multiples of 16 positions, so 16
 // positions of one head lie in one block and travel as one tiled bulk copy (or, where a head is no whole number of panels,
@@ -564,44 +578,49 @@ struct Shared {          // beside the ring
 template <class S, bool TILED>
 struct Feeder {
     // whether a stage's barrier also counts every lane of a copying warp, for copies that are not bulk copies
-    static constexpr bool kLaneArrivals = !TILED || S::DT == PSMC_F8;
+    static __host__ __device__ constexpr bool lane_arrivals(int which) { return !TILED || S::DT == PSMC_F8 || (which == 0 && S::kSlots > 0); }
     struct Asked {
         int in_block;    // lane u: head * block_len + offset in the block, of slice u
         int live;        // lane u: positions of it that lie in the segment
         int tile, head, row, p, p1;  // not TILED: the step itself
         bool any;        // whether there is a step at all
+        int begins;      // the item that begins with it, or -1
     };
     Walk<S> walk;
     Asked first, second;
-    int items;           // put into the queue so far
+    int items;           // begun so far
     int asked;           // steps asked for so far
     int worker, lane;
     int which;           // 0: keys, 1: values
 
-    __device__ __forceinline__ void open_item(const AttendArgs& g, Shared<S>& sh) {
+    __device__ __forceinline__ void open_item(Shared<S>& sh, const AttendArgs& g) {
         Item& it = sh.queue[items % kQueue];
         if (lane == 0) it.head_part = walk.item(g.l, worker);
         if (walk.mask >> lane & 1) it.rows[__popc(walk.mask & ((1u << lane) - 1))] = (uint8_t)lane;
         __syncwarp();
-        ++items;
-        if (lane == 0) {
-            __threadfence_block();
-            *const_cast<volatile int*>(&sh.opened) = items;
-        }
-        // the queries will be loaded by the warps that need them; brought near by now, they cost them little
-        const int lines = (g.c.D * (S::DT == PSMC_F32 ? 4 : 2) + 127) / 128;
-        for (int x = lane; x < walk.nq * lines; x += 32) {
-            const int in_tile = x / lines, qi = walk.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
-            const int64_t row = walk.tile * kTileRows + it.rows[rank], qh = walk.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
-            const char* at = static_cast<const char*>(g.a.q.data) + (row * g.a.q.stride_row + qh * g.a.q.stride_head) * (S::DT == PSMC_F32 ? 4 : 2);
-            asm volatile("prefetch.global.L1 [%0];" ::"l"(at + (x - in_tile * lines) * 128));
+    }
+    // an item's queries, to the slot of the stage that its first step goes to
+    __device__ __forceinline__ void copy_queries(const AttendArgs& g, const Item& it, char* slot) {
+        const int units = g.c.D / 8;
+        const ItemHead& h = it.head_part;
+        for (int x = lane; x < h.nq * units; x += 32) {
+            const int in_tile = div_by(x, g.by_units), u = x - in_tile * units;
+            int row, qh;
+            place<S>(g, h, it.rows, in_tile, &row, &qh);
+            const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(g.a.q.data) + (int64_t)row * g.a.q.stride_row + (int64_t)qh * g.a.q.stride_head;
+            copy16(smem_of(slot + in_tile * S::kQueryRow + u * 16), q + u * 8, 16);
         }
     }
     __device__ __forceinline__ Asked ask(const AttendArgs& g, Shared<S>& sh) {
         Asked q{};
         q.any = !walk.done;
+        q.begins = -1;
         if (!walk.done) {
-            if (walk.s == walk.s_first && which == 0) open_item(g, sh);
+            if (walk.s == walk.s_first) {
+                q.begins = items;
+                if (which == 0) open_item(sh, g);
+                ++items;
+            }
             const int p = walk.p0 + walk.s * S::kStep, row = walk.tile * kTileRows + __ffs(walk.mask) - 1;
             if (TILED) {
                 const int mine = p + lane * 16;
@@ -628,6 +647,12 @@ struct Feeder {
         char* stage = ring + to * S::kStage + which * S::kHalf;
         uint8_t* scales = reinterpret_cast<uint8_t*>(ring) + to * S::kStage + 2 * S::kHalf + which * S::kScales;
         const char* pool = which ? g.c.v : g.c.k;
+        if (S::kSlots > 0 && which == 0) {
+            if (first.begins >= 0 && g.q_units) {
+                const Item& it = sh.queue[first.begins % kQueue];
+                if (it.head_part.nq <= S::kSlotQueries) copy_queries(g, it, ring + S::kStages * S::kStage + to * S::kSlots);
+            }
+        }
         if (TILED) {
             copies_wait<1>();  // the entries asked for last may still be on their way
             const int entry = first.live > 0 ? sh.entries[which][(asked - 2) % 4][lane] : -1;
@@ -649,7 +674,7 @@ struct Feeder {
                 }
                 if (S::DT == PSMC_F8) copy16(smem_of(scales + lane * 16), pool + (int64_t)entry * g.c.blk_bytes + g.c.scale_at + first.in_block, 16);
             }
-            if (S::DT == PSMC_F8) copies_arrive(&sh.full[to]);
+            if (lane_arrivals(which)) copies_arrive(&sh.full[to]);
         } else {
             constexpr int kPerRow = S::kPanels * (kPanel / 16);
             const int per_row = g.c.D * S::kElem / 16;
@@ -708,7 +733,7 @@ struct Feeder {
                     if (which == 0) sh.valid[stage][0] = kEnd;
                     mbar_expect_tx(&sh.full[stage], 0);
                 }
-                if (kLaneArrivals) copies_arrive(&sh.full[stage]);
+                if (lane_arrivals(which)) copies_arrive(&sh.full[stage]);
                 return;
             }
             issue(g, stage, ring, sh);
@@ -762,26 +787,43 @@ struct Division {
     }
 };
 
-// row and query head of query `in_tile` of an item
-template <class S>
-__device__ __forceinline__ void place(const AttendArgs& g, const ItemHead& it, const uint8_t* rows, int in_tile, int* row, int* qh) {
-    const int qi = it.qt * (kGroups * S::kGroup) + in_tile, rank = div_by(qi, g.by_ratio);
-    *row = it.tile * kTileRows + rows[rank];
-    *qh = it.head * g.l.ls.ratio + qi - rank * g.l.ls.ratio;
-}
-
 // ---- the arithmetic of one warp: NT tiles of 8 queries against tiles of 16 positions
-template <class S>
+template <class S, int NT>
 struct RawQueries {      // lane (gq, t) holds components of query gq of each tile
-    uint32_t x[2][S::DP / 16][2];
+    uint32_t x[NT][S::DP / 16][2];
 };
-template <class S>
-__device__ __forceinline__ void load_queries(const AttendArgs& g, const ItemHead& it, const uint8_t* rows, RawQueries<S>& q, const Pipe& pp) {
+// from a slot that holds this warp's queries (its other rows hold anything: what comes of them stays in columns of their own)
+template <class S, int NT>
+__device__ __forceinline__ void fetch_queries(uint32_t slot, RawQueries<S, NT>& q, int lane) {
+    if (S::DT != PSMC_F8) {
+        // four 8 x 8 tiles at a time: lanes 8 i .. 8 i + 7 name the rows of tile i
+        const uint32_t at = slot + (lane & 7) * S::kQueryRow + (lane >> 3) * 16;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int ks = 0; ks < S::DP / 16; ks += 2) {
+                uint32_t r[4];
+                load_tiles(r, at + j * 8 * S::kQueryRow + ks * 32);
+                q.x[j][ks][0] = r[0];
+                q.x[j][ks][1] = r[1];
+                q.x[j][ks + 1][0] = r[2];
+                q.x[j][ks + 1][1] = r[3];
+            }
+    } else {
+        const uint32_t at = slot + (lane >> 2) * S::kQueryRow + (lane & 3) * 8;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int ks = 0; ks < S::DP / 16; ++ks)
+                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(q.x[j][ks][0]), "=r"(q.x[j][ks][1]) : "r"(at + j * 8 * S::kQueryRow + ks * 32));
+    }
+}
+template <class S, int NT>
+__device__ __forceinline__ void load_queries(const AttendArgs& g, const ItemHead& it, const uint8_t* rows, RawQueries<S, NT>& q, const Pipe& pp) {
     const Division dv(it.nq, S::kGroup, S::kSlices, pp.warp);
     const int t = pp.lane & 3, gq = pp.lane >> 2, q0 = dv.group * S::kGroup;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        if (j > 0 && it.nq <= 8) break;
+    for (int j = 0; j < NT; ++j) {
         const int in_tile = q0 + j * 8 + gq;
         const uint16_t* src = nullptr;
         if (in_tile < it.nq) {
@@ -809,7 +851,7 @@ struct Tiles {
     float sc[NT][2];      // queries 2t, 2t + 1 of each tile: factor from product to score in log2 units
     float o[NT][kDt][4], ref[NT][2], sum[NT][2];
 
-    __device__ __forceinline__ void clear(RawQueries<S>& q, float to_log2, int lane) {
+    __device__ __forceinline__ void clear(RawQueries<S, NT>& q, float to_log2, int lane) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             ref[j][0] = ref[j][1] = -INFINITY;
@@ -845,7 +887,7 @@ struct Tiles {
     // MT slices: keys[m], vals[m]: shared addresses of their 16 rows; valid[m]: which of them hold something; k_scale[m],
     // v_byte[m]: lane p's scales (8-bit)
     template <int MT>
-    __device__ __forceinline__ void step(const RawQueries<S>& q, const uint32_t (&keys)[MT], const uint32_t (&vals)[MT], const uint32_t (&valid)[MT],
+    __device__ __forceinline__ void step(const RawQueries<S, NT>& q, const uint32_t (&keys)[MT], const uint32_t (&vals)[MT], const uint32_t (&valid)[MT],
                                          const float (&k_scale)[MT], const int (&v_byte)[MT], int lane) {
         const int gq = lane >> 2;
         float s[MT][NT][4], s2[MT][NT][4];  // two chains, so that the products of one tile wait less for each other
@@ -921,6 +963,8 @@ struct Tiles {
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
+                    // each query by itself: another one of the tile, or a column that none uses, does not change its roundings
+                    if (!(top > ref[j][i] + kSlack)) top = ref[j][i];
                     const float f = top == ref[j][i] ? 1.f : ex2(ref[j][i] - top);
                     ref[j][i] = top;
                     sum[j][i] *= f;
@@ -1019,6 +1063,7 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& 
                                            const uint8_t* rows, int first, const Pipe& pp, int index) {
     using T = typename PoolIo<S::DT>::type;
     constexpr int kPitch = S::DP + 4;
+#pragma unroll 2
     for (int u = 0; u < 2 * dv.groups; ++u) {  // the warps share the queries evenly
         const int x = pp.warp * 2 * dv.groups + u, grp = x >> 3, ql = x & 7, in_tile = grp * S::kGroup + first + ql;
         if (in_tile >= it.nq || first + ql >= S::kGroup) continue;
@@ -1029,8 +1074,8 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& 
                 top = fmaxf(top, sh.stats[index & 1][z * dv.groups + grp][first + ql].x);
                 total += sh.scaled[z * dv.groups + grp][first + ql];
             }
-        int row, qh;
-        place<S>(g, it, rows, in_tile, &row, &qh);
+        int row = 0, qh = 0;
+        if (it.alone) place<S>(g, it, rows, in_tile, &row, &qh);
         const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
         for (int i = 0; i < (S::DP + 127) / 128; ++i) {
@@ -1060,10 +1105,9 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& 
     }
 }
 
-// One item, from its queries to its result.  NT: tiles of 8 queries per warp.  has_q: the queries have been loaded already;
-// afterwards, whether the next item's have.  false: a wait ran out.
+// One item, from its queries to its result.  NT: tiles of 8 queries per warp.  false: a wait ran out.
 template <class S, bool TILED, int NT>
-__device__ __forceinline__ bool run_item(const AttendArgs& g, RawQueries<S>& q, bool& has_q, Pipe& pp, Shared<S>& sh, int index) {
+__device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S>& sh, int index) {
     using Ti = Tiles<S, NT>;
     constexpr bool kF8 = S::DT == PSMC_F8;
     constexpr int kMost = NT == 1 || S::DP <= 128 ? S::kPair : 1;  // slices at a time
@@ -1073,7 +1117,11 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, RawQueries<S>& q, 
     const Division dv(it.nq, S::kGroup, S::kSlices, warp);
     const bool busy = dv.slice < dv.slices && dv.group * S::kGroup < it.nq;
     bool fine = true;
-    if (!has_q) load_queries<S>(g, it, rows, q, pp);
+    RawQueries<S, NT> q;
+    if (S::kSlots > 0 && g.q_units && it.nq <= S::kSlotQueries)
+        fetch_queries<S, NT>(smem_of(pp.ring + S::kStages * S::kStage + pp.stage * S::kSlots) + dv.group * S::kGroup * S::kQueryRow, q, lane);
+    else
+        load_queries<S, NT>(g, it, rows, q, pp);
     Ti ti;
     ti.clear(q, g.a.scale * kLog2e, lane);
     int used = pp.stage;  // the stage worked on last: kept until the result is written, which passes through it
@@ -1117,14 +1165,6 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, RawQueries<S>& q, 
             }
         }
         next_stage<S>(pp);
-    }
-    // ---- the next item's queries travel while this one's result is put together, if the copying warp has got to it
-    has_q = false;
-    if (fine && *const_cast<volatile int*>(&sh.opened) > index + 1) {
-        __threadfence_block();
-        const Item& next = sh.queue[(index + 1) % kQueue];
-        load_queries<S>(g, next.head_part, next.rows, q, pp);
-        has_q = true;
     }
     // ---- sums over the lanes that hold parts of them, then over the slices
 #pragma unroll
@@ -1177,12 +1217,14 @@ __device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe&
     pp.lane = threadIdx.x & 31;
     pp.warp = threadIdx.x >> 5;
     pp.worker = blockIdx.x;
+    if (S::kSlots > 0 && g.c.D < S::DP)  // components beyond the head: never copied, always zero
+        for (int i = threadIdx.x; i < S::kStages * S::kSlots / 16; i += kThreads)
+            reinterpret_cast<uint4*>(pp.ring + S::kStages * S::kStage)[i] = uint4{0, 0, 0, 0};
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
-            mbar_init(&sh.full[i], 2 * (Feeder<S, TILED>::kLaneArrivals ? 33 : 1));
+            mbar_init(&sh.full[i], (Feeder<S, TILED>::lane_arrivals(0) ? 33 : 1) + (Feeder<S, TILED>::lane_arrivals(1) ? 33 : 1));
             mbar_init(&sh.empty[i], kWarps);
         }
-        sh.opened = 0;
         fence_async_smem();
     }
     __syncthreads();
@@ -1209,14 +1251,12 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_kernel(const 
     static_assert(sizeof(sh) <= S::kBeside, "beside the ring");
     Pipe pp;
     if (!open_pipe<S, TILED>(g, smem, pp, sh)) return;
-    RawQueries<S> q;
-    bool has_q = false;
     for (int index = 0;; ++index) {
         bool fine = landed<S>(pp, sh);
         if (fine) {
             if (sh.valid[pp.stage][0] == kEnd) return;
-            fine = sh.queue[index % kQueue].head_part.nq <= 8 ? run_item<S, TILED, 1>(g, q, has_q, pp, sh, index)
-                                                              : run_item<S, TILED, 2>(g, q, has_q, pp, sh, index);
+            fine = sh.queue[index % kQueue].head_part.nq <= 8 ? run_item<S, TILED, 1>(g, pp, sh, index)
+                                                              : run_item<S, TILED, 2>(g, pp, sh, index);
         }
         if (!fine) {
             give_up<S>(g, pp, sh);
@@ -1472,8 +1512,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
             const int qi = __popc(sg.mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / qt_size;
             const int steps = steps_of(ls, sg.p0, sg.p1);
             const int w = step_cost(ls.group, min(qt_size, __popc(sg.mask) * ls.ratio - qt * qt_size));
-            const int64_t a = b.before + head * tp.cost + sg.start + (int64_t)qt * steps * step_cost(ls.group, qt_size);
-            const int64_t k0 = quotient(a, b.share), k1 = quotient(a + (int64_t)steps * w - 1, b.share);
+            const int64_t a = b.before + head * tp.cost + sg.start + (int64_t)qt * ((int64_t)steps * step_cost(ls.group, qt_size) + kItemCost);
+            const int64_t k0 = quotient(a, b.share), k1 = quotient(a + (int64_t)steps * w + kItemCost - 1, b.share);
             const int64_t first = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio) + (int64_t)sg.before * ls.ratio + qi;
             for (int64_t kb = k0; kb <= k1; kb += 32) {
                 const int64_t k = kb + lane;
@@ -1586,7 +1626,9 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.by_block = fast_div(c.block_len);
     g.l.ls = LineShape{S::kStep, S::kGroup, a.Hq / c.H, c.H};
     g.by_ratio = fast_div(g.l.ls.ratio);
+    g.by_units = fast_div(c.D < 8 ? 1 : c.D / 8);
     g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
+    g.q_units = ((uint64_t)(uintptr_t)a.q.data % 16 == 0 && a.q.stride_row % 8 == 0 && a.q.stride_head % 8 == 0 && c.D % 8 == 0) ? 1 : 0;
     TilePlan* plans = reinterpret_cast<TilePlan*>(scratch + sc.plans);
     g.l.plans = plans;
     g.l.stat = reinterpret_cast<float2*>(scratch + sc.stat);
