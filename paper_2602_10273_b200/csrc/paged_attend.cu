@@ -557,7 +557,6 @@ struct Shared {          // beside the ring
     int entries[2][4][S::kSlices];       // table entries of the steps asked for, of either copying warp
     Item queue[kQueue];
     float2 stats[2][kWarps][16];         // {reference, sum} of each warp's queries, of this item and the one before
-    float scaled[kWarps][16];            // its sum as a share of the largest reference of the query's slices
 };
 
 // row and query head of query `in_tile` of an item
@@ -1055,52 +1054,77 @@ __device__ __forceinline__ void clear_rows(char* vals, uint32_t valid, int lane)
     __syncwarp();
 }
 
-// One tile of 8 queries of every warp, outputs in `carry` [warp][query][DP + 4] as shares of the largest reference of their
-// slices: summed over the slices and written, to the queries' rows or as partial results, 16 bytes per lane.  first: the
-// tile's first query within a warp's group.
+// One tile of 8 queries of every warp, outputs in `carry` [warp][query][DP + 4], each relative to its own slice's reference:
+// summed over the slices and written, to the queries' rows or as partial results, 16 bytes per lane.  first: the tile's
+// first query within a warp's group.
 template <class S>
-__device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& it, const Division& dv, const float* carry, const Shared<S>& sh,
-                                           const uint8_t* rows, int first, const Pipe& pp, int index) {
+__device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& it, const Division& dv, const float* carry, const float2 (*stats)[16],
+                                           const uint8_t* rows, int first, const Pipe& pp) {
     using T = typename PoolIo<S::DT>::type;
-    constexpr int kPitch = S::DP + 4;
-#pragma unroll 2
-    for (int u = 0; u < 2 * dv.groups; ++u) {  // the warps share the queries evenly
-        const int x = pp.warp * 2 * dv.groups + u, grp = x >> 3, ql = x & 7, in_tile = grp * S::kGroup + first + ql;
-        if (in_tile >= it.nq || first + ql >= S::kGroup) continue;
-        float top = -INFINITY, total = 0.f;
+    constexpr int kPitch = S::DP + 4, kOwn = (S::DP + 127) / 128;
+#pragma unroll 1
+    for (int u = 0; u < 2 * dv.groups; u += 2) {  // the warps share the queries evenly, and take two at a time
+        float4 o[2][kOwn];
+        float top[2], total[2];
+        bool ok[2];
+        int in_tile[2];
 #pragma unroll
-        for (int z = 0; z < kWarps; ++z)
-            if (z < dv.slices) {
-                top = fmaxf(top, sh.stats[index & 1][z * dv.groups + grp][first + ql].x);
-                total += sh.scaled[z * dv.groups + grp][first + ql];
+        for (int v = 0; v < 2; ++v) {
+            const int x = pp.warp * 2 * dv.groups + u + v, grp = x >> 3, ql = x & 7;
+            in_tile[v] = grp * S::kGroup + first + ql;
+            ok[v] = in_tile[v] < it.nq && first + ql < S::kGroup;
+            float2 st[kWarps];
+            top[v] = -INFINITY;
+            total[v] = 0.f;
+#pragma unroll
+            for (int z = 0; z < kWarps; ++z) {
+                st[z] = float2{-INFINITY, 0.f};
+                if (z < dv.slices) st[z] = stats[z * dv.groups + grp][first + ql];
+                top[v] = fmaxf(top[v], st[z].x);
             }
-        int row = 0, qh = 0;
-        if (it.alone) place<S>(g, it, rows, in_tile, &row, &qh);
-        const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-        for (int i = 0; i < (S::DP + 127) / 128; ++i) {
-            const int d = pp.lane * 4 + i * 128;
-            if (d >= g.c.D) continue;
-            float4 o = float4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < kOwn; ++i) o[v][i] = float4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int z = 0; z < kWarps; ++z)
                 if (z < dv.slices) {
-                    const float4 y = *reinterpret_cast<const float4*>(carry + ((z * dv.groups + grp) * 8 + ql) * kPitch + d);
-                    o.x += y.x;
-                    o.y += y.y;
-                    o.z += y.z;
-                    o.w += y.w;
+                    // (a factor of zero keeps a NaN that came with the values)
+                    const float f = st[z].x == top[v] ? 1.f : (st[z].x == -INFINITY ? 0.f : ex2(st[z].x - top[v]));
+                    total[v] = fmaf(st[z].y, f, total[v]);
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        const int d = pp.lane * 4 + i * 128;
+                        if (d >= S::DP) continue;
+                        const float4 y = *reinterpret_cast<const float4*>(carry + ((z * dv.groups + grp) * 8 + ql) * kPitch + d);
+                        o[v][i].x = fmaf(y.x, f, o[v][i].x);
+                        o[v][i].y = fmaf(y.y, f, o[v][i].y);
+                        o[v][i].z = fmaf(y.z, f, o[v][i].z);
+                        o[v][i].w = fmaf(y.w, f, o[v][i].w);
+                    }
                 }
-            if (it.alone) {
-                o = float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
-                put4(static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head + d, o);
-            } else {
-                *reinterpret_cast<float4*>(g.l.part + (it.slot + in_tile) * g.c.D + d) = o;
-            }
         }
-        if (pp.lane == 0) {
-            if (!it.alone) g.l.stat[it.slot + in_tile] = float2{top, total};
-            else if (g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total == 0.f ? -INFINITY : kLn2 * (top + log2f(total));
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            if (!ok[v]) continue;
+            if (!it.alone) {
+                float* part = g.l.part + (it.slot + in_tile[v]) * g.c.D;
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    const int d = pp.lane * 4 + i * 128;
+                    if (d < g.c.D) *reinterpret_cast<float4*>(part + d) = o[v][i];
+                }
+                if (pp.lane == 0) g.l.stat[it.slot + in_tile[v]] = float2{top[v], total[v]};
+                continue;
+            }
+            int row, qh;
+            place<S>(g, it, rows, in_tile[v], &row, &qh);
+            const float inv = total[v] == 0.f ? 0.f : 1.f / total[v];
+            T* out = static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                const int d = pp.lane * 4 + i * 128;
+                if (d < g.c.D) put4(out + d, float4{o[v][i].x * inv, o[v][i].y * inv, o[v][i].z * inv, o[v][i].w * inv});
+            }
+            if (pp.lane == 0 && g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total[v] == 0.f ? -INFINITY : kLn2 * (top[v] + log2f(total[v]));
         }
     }
 }
@@ -1178,29 +1202,20 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S
             ti.sum[j][i] = x;
             if (gq == 0) sh.stats[index & 1][warp][j * 8 + 2 * t + i] = float2{ti.ref[j][i], x};
         }
-    sync_warps();  // also: everyone is done with the last step's stage, which now carries the outputs
     float* carry = reinterpret_cast<float*>(pp.ring + used * S::kStage);
     constexpr int kPitch = S::DP + 4;
+    sync_warps();  // everyone is done with the last step's stage, which now carries the outputs
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         if (busy)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int z = 0; z < kWarps; ++z)
-                    if (z < dv.slices) top = fmaxf(top, sh.stats[index & 1][z * dv.groups + dv.group][j * 8 + 2 * t + i].x);
-                // (a factor of zero keeps a NaN that came with the values)
-                const float f = ti.ref[j][i] == top ? 1.f : (ti.ref[j][i] == -INFINITY ? 0.f : ex2(ti.ref[j][i] - top));
-                if (gq == 0) sh.scaled[warp][j * 8 + 2 * t + i] = ti.sum[j][i] * f;
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int d = 0; d < Ti::kDt; ++d)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        carry[(warp * 8 + 2 * t + i) * kPitch + Ti::component(d, e, lane)] = ti.o[j][d][2 * e + i] * f;
-            }
+                    for (int e = 0; e < 2; ++e) carry[(warp * 8 + 2 * t + i) * kPitch + Ti::component(d, e, lane)] = ti.o[j][d][2 * e + i];
         sync_warps();
-        write_tile<S>(g, it, dv, carry, sh, rows, j * 8, pp, index);
+        write_tile<S>(g, it, dv, carry, sh.stats[index & 1], rows, j * 8, pp);
         if (j + 1 < NT) sync_warps();
     }
     if (TILED) fence_async_smem();
@@ -1390,20 +1405,15 @@ __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, float* qs, flo
         for (int x = 1; x < 16; x <<= 1) sum[u] += __shfl_xor_sync(kFull, sum[u], x);
         if (key == 0 && (NQ == 8 || half == 0)) sh.stats[index & 1][warp][qh4 + u] = float2{ref[u], sum[u]};
     }
-    sync_warps();  // also: everyone is done with the last step's stage, which now carries the outputs
+    sync_warps();  // everyone is done with the last step's stage, which now carries the outputs
     float* carry = reinterpret_cast<float*>(pp.ring + used * S::kStage);
     if (mine > 0)
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            float top = -INFINITY;
-            for (int z = 0; z < dv.slices; ++z) top = fmaxf(top, sh.stats[index & 1][z * dv.groups + dv.group][j].x);
-            const float own = sh.stats[index & 1][warp][j].x, f = own == top ? 1.f : (own == -INFINITY ? 0.f : exp2f(own - top));
-            if (lane == 0) sh.scaled[warp][j] = sh.stats[index & 1][warp][j].y * f;
+        for (int j = 0; j < NQ; ++j)
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i) carry[(warp * 8 + j) * (S::DP + 4) + lane + 32 * i] = o[j][i] * f;
-        }
+            for (int i = 0; i < kOwn; ++i) carry[(warp * 8 + j) * (S::DP + 4) + lane + 32 * i] = o[j][i];
     sync_warps();
-    write_tile<S>(g, it, dv, carry, sh, rows, 0, pp, index);
+    write_tile<S>(g, it, dv, carry, sh.stats[index & 1], rows, 0, pp);
     if (TILED) fence_async_smem();
     release<S>(sh, used, lane);
     return fine;
@@ -1437,10 +1447,10 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_f32_kernel(co
 constexpr int kMaxWorkers = 2 * kSMs;
 constexpr int kJoinThreads = 128;
 
-template <int DT, int WPQ>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ AttendArgs g) {
+template <int DT, int WPQ, int OWN>
+__global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_kernel(const __grid_constant__ AttendArgs g) {
     using T = typename PoolIo<DT>::type;
-    constexpr int kJoinWarps = kJoinThreads / 32, kQueries = kJoinWarps / WPQ, kOwn = kMaxHeadDim / 128, kList = 32, kBatch = 8;
+    constexpr int kJoinWarps = kJoinThreads / 32, kQueries = kJoinWarps / WPQ, kOwn = OWN, kList = 32, kBatch = OWN == 1 ? 8 : 4;
     __shared__ int64_t slots[kJoinWarps][kList];
     __shared__ __align__(16) float acc[WPQ == 1 ? 1 : WPQ][kMaxHeadDim];  // read and written 16 bytes at a time
     __shared__ float2 stats[kJoinWarps];
@@ -1453,9 +1463,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     const TilePlan& tp = g.l.plans[tile];
     const LineShape& ls = g.l.ls;
     const int qt_size = kGroups * ls.group;
-    uint32_t masks[kMaxSegs / 32];
-#pragma unroll
-    for (int i = 0; i < kMaxSegs / 32; ++i) masks[i] = tp.seg[i * 32 + lane].mask;  // those beyond n_segs are not looked at
+    int4 seg = *reinterpret_cast<const int4*>(&tp.seg[lane]);  // (those beyond n_segs are not looked at)
+    int64_t seg_start = tp.seg[lane].start;
     const Bearings b = bearings(g.l, 0, tile, lane);
     const int n_segs = tp.n_segs;
     if (tp.left_out >> in_tile & 1) return;
@@ -1504,17 +1513,24 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
         listed = 0;
     };
 #pragma unroll 1
-    for (int i = 0; i < kMaxSegs / 32; ++i) {
-        uint32_t with = __ballot_sync(kFull, i * 32 + lane < n_segs && (masks[i] >> in_tile & 1));
+    for (int s0 = 0; s0 < n_segs; s0 += 32) {
+        if (s0 > 0) {
+            seg = *reinterpret_cast<const int4*>(&tp.seg[s0 + lane]);
+            seg_start = tp.seg[s0 + lane].start;
+        }
+        uint32_t with = __ballot_sync(kFull, s0 + lane < n_segs && ((uint32_t)seg.x >> in_tile & 1));
         while (with) {
-            const Segment sg = tp.seg[i * 32 + __ffs(with) - 1];
+            const int at = __ffs(with) - 1;
             with &= with - 1;
-            const int qi = __popc(sg.mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / qt_size;
-            const int steps = steps_of(ls, sg.p0, sg.p1);
-            const int w = step_cost(ls.group, min(qt_size, __popc(sg.mask) * ls.ratio - qt * qt_size));
-            const int64_t a = b.before + head * tp.cost + sg.start + (int64_t)qt * ((int64_t)steps * step_cost(ls.group, qt_size) + kItemCost);
+            const uint32_t mask = (uint32_t)__shfl_sync(kFull, seg.x, at);
+            const int p0 = __shfl_sync(kFull, seg.y, at), p1 = __shfl_sync(kFull, seg.z, at), before = __shfl_sync(kFull, seg.w, at);
+            const int64_t start = __shfl_sync(kFull, (long long)seg_start, at);
+            const int qi = __popc(mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / qt_size;
+            const int steps = steps_of(ls, p0, p1);
+            const int w = step_cost(ls.group, min(qt_size, __popc(mask) * ls.ratio - qt * qt_size));
+            const int64_t a = b.before + head * tp.cost + start + (int64_t)qt * ((int64_t)steps * step_cost(ls.group, qt_size) + kItemCost);
             const int64_t k0 = quotient(a, b.share), k1 = quotient(a + (int64_t)steps * w + kItemCost - 1, b.share);
-            const int64_t first = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio) + (int64_t)sg.before * ls.ratio + qi;
+            const int64_t first = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio) + (int64_t)before * ls.ratio + qi;
             for (int64_t kb = k0; kb <= k1; kb += 32) {
                 const int64_t k = kb + lane;
                 const int from = steps_before(k * b.share, a, w, steps);
@@ -1649,8 +1665,9 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     if (e != cudaSuccess) return e;
     // few queries: four warps each, for what may be many partial results of a long row
     const int64_t queries = (int64_t)c.R * a.Hq;
-    if (queries <= 8 * kSMs) return launch_chained(paged_join_kernel<DT, 4>, dim3((unsigned)queries), dim3(kJoinThreads), 0, stream, g);
-    return launch_chained(paged_join_kernel<DT, 1>, dim3((unsigned)((queries + 3) / 4)), dim3(kJoinThreads), 0, stream, g);
+    constexpr int kOwn = DP > 128 ? 2 : 1;
+    if (queries <= 8 * kSMs) return launch_chained(paged_join_kernel<DT, 4, kOwn>, dim3((unsigned)queries), dim3(kJoinThreads), 0, stream, g);
+    return launch_chained(paged_join_kernel<DT, 1, kOwn>, dim3((unsigned)((queries + 3) / 4)), dim3(kJoinThreads), 0, stream, g);
 }
 
 template <int DT>
