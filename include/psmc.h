@@ -357,7 +357,7 @@ psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows
  * positions gets zeros and lse = -inf; rows with skip[r] != 0 are left as they were.  Blocks that several rows share are
  * read once for all of them where they lie within a run of 32 rows.  scratch: psmc_paged_attend_scratch_bytes() bytes,
  * 256-byte aligned, contents irrelevant; calls that may overlap (other streams, graphs replayed side by side) need
- * scratch of their own.  out may not overlap q.  Pools of up to 64 GiB, R * Hq up to 2^27. */
+ * scratch of their own.  out may not overlap q.  max_blocks * block_len and R * Hq up to 2^27. */
 size_t psmc_paged_attend_scratch_bytes(int R, int n_q_heads, int n_kv_heads, int head_dim);
 psmc_status psmc_paged_attend(const psmc_paged_kv* kv, const int32_t* lens, int extra, const uint8_t* skip, int n_q_heads,
                               const psmc_heads* q, const psmc_heads* out, float scale, float* lse, void* scratch,

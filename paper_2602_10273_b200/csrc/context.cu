@@ -687,8 +687,8 @@ psmc_status paged_attend(const PagedView& c, const int32_t* lens, int extra, con
     if (!lens || extra < 0 || Hq < 1 || Hq % c.H != 0 || !heads_ok(q, c.dt) || !heads_ok(out, c.dt)) return PSMC_E_INVAL;
     if (!scratch || (uint64_t)(uintptr_t)scratch % 256 != 0 || scratch_bytes < psmc_paged_attend_scratch_bytes(c.R, Hq, c.H, c.D))
         return PSMC_E_INVAL;
-    // blocks are addressed in 16-byte units of 32 bits, and the workspace's partial results are numbered in 32 bits
-    if ((uint64_t)c.n_blocks * (uint64_t)(c.blk_bytes / 16) > 0xffffffffull || (int64_t)c.R * Hq > (1 << 27)) return PSMC_E_INVAL;
+    // partial results are numbered in 32 bits, and what one tile of rows costs is counted in them
+    if ((int64_t)c.R * Hq > (1 << 27) || (int64_t)c.max_blocks * c.block_len > (1 << 27)) return PSMC_E_INVAL;
     PagedAttend a{};
     a.lens = lens; a.extra = extra; a.skip = skip; a.Hq = Hq; a.q = heads_view(q); a.out = heads_view(out); a.scale = scale;
     a.lse = lse; a.scratch = scratch; a.status = status;

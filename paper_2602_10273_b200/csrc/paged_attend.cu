@@ -56,21 +56,18 @@ struct LineShape {       // how the items of a tile are cut; a pure function of 
     int group;           // queries per warp; a query tile has kGroups times as many
     int ratio, H;
 };
-// What a step costs by its queries: its bytes are the same, and beside them the arithmetic of one or two groups is small.
-__device__ __forceinline__ int step_cost(int group, int nq) {
-    const int groups = (nq + group - 1) / group;
-    return 4 + (groups > 1 ? groups : 0);
-}
-// and an item beside its steps, for putting its result together
-constexpr int kItemCost = 5;
+// Cost of an item on the line: a step's share is the same whether one group of queries meets it or four (its bytes and the
+// instructions that every warp spends on a slice decide), and putting a result together takes as long as two steps or less.
+constexpr int kStepLog2 = 2, kItemCost = 7;
+__host__ __device__ __forceinline__ int64_t item_cost(int steps) { return ((int64_t)steps << kStepLog2) + kItemCost; }
 __device__ __forceinline__ int64_t seg_cost(const LineShape& s, int rows, int steps) {
-    const int nq = rows * s.ratio, qt = s.group * kGroups, full = nq / qt, rem = nq - full * qt;
-    return (int64_t)steps * (full * step_cost(s.group, qt) + (rem ? step_cost(s.group, rem) : 0)) + (full + (rem > 0)) * kItemCost;
+    const int qt = s.group * kGroups;
+    return (rows * s.ratio + qt - 1) / qt * item_cost(steps);
 }
 __device__ __forceinline__ int steps_of(const LineShape& s, int p0, int p1) { return (p1 - p0 + s.step - 1) / s.step; }
 
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
-constexpr int kRun = 8;              // block indices that a warp looks at in one go
+constexpr int kRun = 4;              // block indices that a warp looks at in one go
 constexpr int kWarpSegs = 32;        // segments that may begin in one warp's block indices
 
 __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedView c, const PagedAttend a, const LineShape ls,
@@ -112,7 +109,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
     const int nb = warp_max((n + B - 1) / B);
 
     // How this row stands in block j: positions of it that count, and the block's number, if it has one that exists.
-    const auto live_in = [&](int j) -> int { return (int)min((int64_t)B, max((int64_t)0, n - (int64_t)j * B)); };
+    const auto live_in = [&](int j) -> int { return min(B, max(0, n - j * B)); };
     const auto name_of = [&](int entry, int live) -> int { return live > 0 && entry >= 0 && entry < c.n_blocks ? entry : -1 - lane; };
     // rows that stand alike in a block, this one among them (0: the row ends before it)
     const auto all_like = [&](int name, int live) -> uint32_t {
@@ -135,6 +132,11 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
                 // two sets that meet again are just read apart.  A set splits where some row of it does not stand like its
                 // first row; its pieces are taken off one by one, first rows first.
                 const uint32_t prev = j == 0 ? 0u : set;
+                {
+                    const int lead = set ? __ffs(set) - 1 : lane;
+                    const int lead_name = __shfl_sync(kFull, name, lead), lead_live = __shfl_sync(kFull, live, lead);
+                    if (j > 0 && __all_sync(kFull, set == 0 || (name == lead_name && live == lead_live))) continue;  // as before
+                }
                 uint32_t open = __ballot_sync(kFull, set != 0), mine = set;
                 if (live == 0) set = 0;
                 for (int piece = 0; open && piece < kTileRows; ++piece) {
@@ -181,12 +183,14 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
         if (lane < begun) segs[at + lane] = found[warp][lane];
     }
     __syncthreads();
-    for (int s = threadIdx.x; s < n_segs; s += kPlanThreads) {  // ends where its first row enters another, or ends itself
+    for (int s = warp; s < n_segs; s += kPlanWarps) {  // ends where its first row enters another, or ends itself
         const Found f = segs[s];
-        int end = (n_of[f.lead] + B - 1) / B;
-        for (int o = 0; o < n_segs; ++o)
+        const int len = n_of[f.lead];
+        int end = (len + B - 1) / B;
+        for (int o = lane; o < n_segs; o += 32)
             if (segs[o].from > f.from && (segs[o].mask >> f.lead & 1)) end = min(end, segs[o].from);
-        ends[s] = (int)min((int64_t)end * B, (int64_t)n_of[f.lead]);
+        end = __reduce_min_sync(kFull, end);
+        if (lane == 0) ends[s] = min(end * B, len);
     }
     __syncthreads();
     if (warp == 0) {
@@ -234,9 +238,12 @@ struct Bearings {        // where a tile begins on the line, and how the line is
     int64_t before, share, total;
     int tile;
 };
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {  // x >= 0, y > 0; nearly always small
-    if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
-    return x / y;
+// x / y for x >= 0, y > 0 and a quotient below 2^20: a 32-bit estimate, off by one at most, put right
+__device__ __forceinline__ int quotient(int64_t x, int64_t y) {
+    int q = (int)__fdividef((float)x, (float)y);
+    while ((int64_t)q * y > x) --q;
+    while ((int64_t)(q + 1) * y <= x) ++q;
+    return q;
 }
 // The tile that holds cost unit `worker * share` (or the one asked for), by all lanes of a warp: the costs of all tiles are
 // added up again (16 numbers for 512 rows), which is less than a kernel of its own would take.
@@ -249,8 +256,8 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, (long long)sum, o);
     Bearings b;
     b.total = sum;
-    b.share = quotient(b.total + l.workers - 1, l.workers);
-    if (b.share < 4 + kItemCost) b.share = 4 + kItemCost;  // an item of one step
+    b.share = (int64_t)__ddiv_ru((double)b.total, (double)l.workers) + 1;  // (a little more than an even share does no harm)
+    if (b.share < item_cost(1)) b.share = item_cost(1);
     const int64_t x = worker * b.share;
     int64_t base = 0;
     b.tile = l.n_tiles;
@@ -270,11 +277,11 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
     }
     return b;
 }
-// the steps of an item (first cost unit a, cost w per step) that lie before `bound`
-__device__ __forceinline__ int steps_before(int64_t bound, int64_t a, int w, int steps) {
+// the steps of an item (first cost unit a) that lie before `bound`
+__device__ __forceinline__ int steps_before(int64_t bound, int64_t a, int steps) {
     const int64_t d = bound - a - kItemCost;
     if (d <= 0) return 0;
-    return d >= (int64_t)steps * w ? steps : (int)(((uint32_t)d + (uint32_t)w - 1) / (uint32_t)w);
+    return (int)min((int64_t)steps, (d + (1 << kStepLog2) - 1) >> kStepLog2);
 }
 
 // What the arithmetic of an item has to know of it; the copying side, which is ahead, leaves it in a queue.
@@ -298,7 +305,7 @@ struct Walk {
     int p0, p1;          // positions of the segment
     int nq;              // queries of this query tile
     int before;          // see Segment
-    int w, steps;
+    int steps;
     int s, s_end;        // steps of the item that are this worker's: the next one, and the end
     int s_first;
     bool done;
@@ -326,14 +333,13 @@ struct Walk {
     }
     __device__ __forceinline__ void enter_item(const Line& l, int64_t lo) {
         nq = min(kGroups * S::kGroup, __popc(mask) * l.ls.ratio - qt * kGroups * S::kGroup);
-        w = step_cost(S::kGroup, nq);
-        s_first = s = steps_before(lo, a, w, steps);
-        s_end = steps_before(hi, a, w, steps);
+        s_first = s = steps_before(lo, a, steps);
+        s_end = steps_before(hi, a, steps);
     }
     // the item after this one that has a step for this worker
     __device__ __forceinline__ void next_item(const Line& l) {
         do {
-            a += (int64_t)steps * w + kItemCost;
+            a += item_cost(steps);
             if (a >= hi) {
                 done = true;
                 return;
@@ -389,7 +395,7 @@ struct Walk {
         const int64_t cost = tp.cost, x = lo - b.before;
         n_segs = head_words.x;
         whole = (uint32_t)head_words.y;
-        head = (int)quotient(x, cost);
+        head = quotient(x, cost);
         const int64_t y = x - head * cost;
         si = -1;
         int4 g = seg;
@@ -408,8 +414,8 @@ struct Walk {
             start = tp.seg[s0 + lane].start;
         }
         enter_segment(l, g);
-        const int64_t full = (int64_t)steps * step_cost(S::kGroup, kGroups * S::kGroup) + kItemCost;
-        qt = (int)min((int64_t)(n_qt - 1), quotient(y - first, full));
+        const int64_t full = item_cost(steps);
+        qt = min(n_qt - 1, quotient(y - first, full));
         a = b.before + head * cost + first + qt * full;
         enter_item(l, lo);
         if (s >= s_end) next_item(l);
@@ -536,7 +542,7 @@ struct AttendArgs {
     PagedView c;
     PagedAttend a;
     Line l;
-    FastDiv by_block, by_ratio, by_units;
+    FastDiv by_block, by_ratio, by_units, by_heads;
     int q_words, q_units;  // queries start on 4-byte, 16-byte boundaries throughout
     int one_copy;        // heads are whole panels: a tiled copy brings all panels of a slice
 };
@@ -1443,113 +1449,117 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_f32_kernel(co
 }
 
 // ---------------------------------------------------------------------------------------------------------- join
-// WPQ warps per (row, query head).  Each of them lists the query's partial results, and takes every WPQ-th.
+// WPQ warps per (row, query head); each takes every WPQ-th of the query's partial results, a lane finding one at a time.
 constexpr int kMaxWorkers = 2 * kSMs;
 constexpr int kJoinThreads = 128;
 
 template <int DT, int WPQ, int OWN>
 __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_kernel(const __grid_constant__ AttendArgs g) {
     using T = typename PoolIo<DT>::type;
-    constexpr int kJoinWarps = kJoinThreads / 32, kQueries = kJoinWarps / WPQ, kOwn = OWN, kList = 32, kBatch = OWN == 1 ? 8 : 4;
-    __shared__ int64_t slots[kJoinWarps][kList];
+    constexpr int kJoinWarps = kJoinThreads / 32, kQueries = kJoinWarps / WPQ, kOwn = OWN, kBatch = OWN == 1 ? 8 : 4;
     __shared__ __align__(16) float acc[WPQ == 1 ? 1 : WPQ][kMaxHeadDim];  // read and written 16 bytes at a time
     __shared__ float2 stats[kJoinWarps];
     chain_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub_warp = warp % WPQ;
-    const int64_t item = (int64_t)blockIdx.x * kQueries + warp / WPQ;
-    if (item >= (int64_t)g.c.R * g.a.Hq) return;  // the warps of a query agree
-    const int row = (int)(item / g.a.Hq), qh = (int)(item - (int64_t)row * g.a.Hq);
-    const int tile = row / kTileRows, in_tile = row % kTileRows, head = qh / g.l.ls.ratio, sub = qh - head * g.l.ls.ratio;
+    const int item = blockIdx.x * kQueries + warp / WPQ;
+    if (item >= g.c.R * g.a.Hq) return;  // the warps of a query agree
+    const int row = div_by(item, g.by_heads), qh = item - row * g.a.Hq;
+    const int tile = row / kTileRows, in_tile = row % kTileRows, head = div_by(qh, g.by_ratio), sub = qh - head * g.l.ls.ratio;
     const TilePlan& tp = g.l.plans[tile];
     const LineShape& ls = g.l.ls;
-    const int qt_size = kGroups * ls.group;
+    constexpr int kGroup = DT == PSMC_F32 ? 8 : 16, kTileQueries = kGroups * kGroup;
     int4 seg = *reinterpret_cast<const int4*>(&tp.seg[lane]);  // (those beyond n_segs are not looked at)
     int64_t seg_start = tp.seg[lane].start;
     const Bearings b = bearings(g.l, 0, tile, lane);
     const int n_segs = tp.n_segs;
     if (tp.left_out >> in_tile & 1) return;
+    const int64_t line_at = b.before + head * tp.cost, tile_slots = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio);
 
     float top = -INFINITY, total = 0.f;
     float4 o[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) o[i] = float4{0.f, 0.f, 0.f, 0.f};
-    int listed = 0, seen = 0;  // in this warp's list; of the query altogether
-    // the listed results, at most kList, into the running ones: the largest reference decides, the others' weights are
-    // 2^(their reference - it)
-    const auto take = [&] {
-        __syncwarp();
-        for (int i0 = 0; i0 < listed; i0 += kBatch) {
-            const int n = min(kBatch, listed - i0);
-            float2 st = float2{-INFINITY, 0.f};
-            if (lane < n) st = g.l.stat[slots[warp][i0 + lane]];
-            float4 x[kBatch][kOwn];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-                for (int i = 0; i < kOwn; ++i) {
-                    const int d = lane * 4 + i * 128;
-                    x[u][i] = float4{0.f, 0.f, 0.f, 0.f};
-                    if (u < n && d < g.c.D) x[u][i] = *reinterpret_cast<const float4*>(g.l.part + slots[warp][i0 + u] * g.c.D + d);
-                }
-            const float high = fmaxf(top, warp_max(st.x)), keep = top == high ? 1.f : exp2f(top - high);
-            const float f = st.x == -INFINITY ? 0.f : (st.x == high ? 1.f : exp2f(st.x - high));
-            total = fmaf(total, keep, warp_sum(lane < n ? st.y * f : 0.f));
-            top = high;
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) o[i] = float4{o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep};
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const float fu = __shfl_sync(kFull, f, u);
-#pragma unroll
-                for (int i = 0; i < kOwn; ++i) {
-                    o[i].x = fmaf(fu, x[u][i].x, o[i].x);
-                    o[i].y = fmaf(fu, x[u][i].y, o[i].y);
-                    o[i].z = fmaf(fu, x[u][i].z, o[i].z);
-                    o[i].w = fmaf(fu, x[u][i].w, o[i].w);
-                }
-            }
-        }
-        __syncwarp();
-        listed = 0;
-    };
 #pragma unroll 1
     for (int s0 = 0; s0 < n_segs; s0 += 32) {
         if (s0 > 0) {
             seg = *reinterpret_cast<const int4*>(&tp.seg[s0 + lane]);
             seg_start = tp.seg[s0 + lane].start;
         }
-        uint32_t with = __ballot_sync(kFull, s0 + lane < n_segs && ((uint32_t)seg.x >> in_tile & 1));
-        while (with) {
-            const int at = __ffs(with) - 1;
-            with &= with - 1;
-            const uint32_t mask = (uint32_t)__shfl_sync(kFull, seg.x, at);
-            const int p0 = __shfl_sync(kFull, seg.y, at), p1 = __shfl_sync(kFull, seg.z, at), before = __shfl_sync(kFull, seg.w, at);
-            const int64_t start = __shfl_sync(kFull, (long long)seg_start, at);
-            const int qi = __popc(mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / qt_size;
-            const int steps = steps_of(ls, p0, p1);
-            const int w = step_cost(ls.group, min(qt_size, __popc(mask) * ls.ratio - qt * qt_size));
-            const int64_t a = b.before + head * tp.cost + start + (int64_t)qt * ((int64_t)steps * step_cost(ls.group, qt_size) + kItemCost);
-            const int64_t k0 = quotient(a, b.share), k1 = quotient(a + (int64_t)steps * w + kItemCost - 1, b.share);
-            const int64_t first = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio) + (int64_t)before * ls.ratio + qi;
-            for (int64_t kb = k0; kb <= k1; kb += 32) {
-                const int64_t k = kb + lane;
-                const int from = steps_before(k * b.share, a, w, steps);
-                const bool has = k <= k1 && from < steps_before((k + 1) * b.share, a, w, steps);  // a share may lie between two steps
-                const uint32_t who = __ballot_sync(kFull, has);
-                const int mine_at = seen + __popc(who & ((1u << lane) - 1));
-                const bool keep = has && mine_at % WPQ == sub_warp;
-                const uint32_t kept = __ballot_sync(kFull, keep);
-                if (listed + __popc(kept) > kList) take();
-                if (keep)
-                    slots[warp][listed + __popc(kept & ((1u << lane) - 1))] =
-                        from == 0 ? first : g.l.first_rest + k * qt_size + (qi - qt * qt_size);
-                listed += __popc(kept);
-                seen += __popc(who);
+        // a lane per segment: the shares k0 .. k0 + n - 1 that have, or might have, a part of this query's item
+        const uint32_t mask = (uint32_t)seg.x;
+        int k0 = 0, n = 0, steps = 0, in_item = 0;
+        int64_t a = 0, first = 0;
+        if (s0 + lane < n_segs && (mask >> in_tile & 1)) {
+            const int qi = __popc(mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / kTileQueries;
+            in_item = qi - qt * kTileQueries;
+            steps = steps_of(ls, seg.y, seg.z);
+            a = line_at + seg_start + qt * item_cost(steps);
+            first = tile_slots + (int64_t)seg.w * ls.ratio + qi;
+            k0 = quotient(a, b.share);
+            n = quotient(a + item_cost(steps) - 1, b.share) - k0 + 1;
+            // in place already: the row's only segment, all of it in one share
+            if (tp.whole >> in_tile & 1)
+                for (int k = k0; k < k0 + n && k < k0 + 3; ++k)
+                    if (steps_before(k * b.share, a, steps) == 0 && steps_before((k + 1) * b.share, a, steps) == steps) n = -1;
+        }
+        if (__any_sync(kFull, n < 0)) return;
+        const int upto = warp_scan_incl(n, lane), all = __shfl_sync(kFull, upto, 31);
+#pragma unroll 1
+        for (int r = 0; r < all; r += 32 * WPQ) {
+            const int e = r + lane * WPQ + sub_warp;
+            int at = 0;  // the lane whose segment entry e belongs to: the first with upto > e
+#pragma unroll
+            for (int step = 16; step > 0; step >>= 1)
+                if (__shfl_sync(kFull, upto, at + step - 1) <= e) at += step;
+            at = min(at, 31);
+            const int k = __shfl_sync(kFull, k0, at) + e - (__shfl_sync(kFull, upto, at) - __shfl_sync(kFull, n, at));
+            const int64_t ea = __shfl_sync(kFull, (long long)a, at), efirst = __shfl_sync(kFull, (long long)first, at);
+            const int esteps = __shfl_sync(kFull, steps, at), ein = __shfl_sync(kFull, in_item, at);
+            int64_t slot = -1;
+            float2 st = float2{-INFINITY, 0.f};
+            if (e < all) {
+                const int from = steps_before(k * b.share, ea, esteps);
+                if (from < steps_before((k + 1) * b.share, ea, esteps))  // (a share may lie between two steps)
+                    slot = from == 0 ? efirst : g.l.first_rest + (int64_t)k * kTileQueries + ein;
+            }
+            if (slot >= 0) st = g.l.stat[slot];
+            // into the running result: the largest reference decides, the others' weights are 2^(their reference - it)
+            const float high = fmaxf(top, warp_max(st.x)), keep = top == high ? 1.f : exp2f(top - high);
+            const float f = st.x == -INFINITY ? 0.f : (st.x == high ? 1.f : exp2f(st.x - high));
+            total = fmaf(total, keep, warp_sum(st.y * f));
+            top = high;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) o[i] = float4{o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep};
+            uint32_t have = __ballot_sync(kFull, slot >= 0);
+            while (have) {
+                float4 x[kBatch][kOwn];
+                float fu[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int from = have ? __ffs(have) - 1 : -1;
+                    have &= have - 1;
+                    const int64_t su = __shfl_sync(kFull, (long long)slot, from & 31);
+                    fu[u] = __shfl_sync(kFull, f, from & 31);
+                    if (from < 0) fu[u] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        const int d = lane * 4 + i * 128;
+                        x[u][i] = float4{0.f, 0.f, 0.f, 0.f};
+                        if (from >= 0 && d < g.c.D) x[u][i] = *reinterpret_cast<const float4*>(g.l.part + su * g.c.D + d);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        o[i].x = fmaf(fu[u], x[u][i].x, o[i].x);
+                        o[i].y = fmaf(fu[u], x[u][i].y, o[i].y);
+                        o[i].z = fmaf(fu[u], x[u][i].z, o[i].z);
+                        o[i].w = fmaf(fu[u], x[u][i].w, o[i].w);
+                    }
             }
         }
     }
-    if (seen == 1 && (tp.whole >> in_tile & 1)) return;  // already in place
-    take();
     if (WPQ > 1) {
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) *reinterpret_cast<float4*>(&acc[sub_warp][lane * 4 + i * 128]) = o[i];
@@ -1642,6 +1652,7 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.by_block = fast_div(c.block_len);
     g.l.ls = LineShape{S::kStep, S::kGroup, a.Hq / c.H, c.H};
     g.by_ratio = fast_div(g.l.ls.ratio);
+    g.by_heads = fast_div(a.Hq);
     g.by_units = fast_div(c.D < 8 ? 1 : c.D / 8);
     g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
     g.q_units = ((uint64_t)(uintptr_t)a.q.data % 16 == 0 && a.q.stride_row % 8 == 0 && a.q.stride_head % 8 == 0 && c.D % 8 == 0) ? 1 : 0;
