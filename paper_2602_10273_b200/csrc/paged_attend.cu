@@ -56,13 +56,26 @@ struct LineShape {       // how the items of a tile are cut; a pure function of 
     int group;           // queries per warp; a query tile has kGroups times as many
     int ratio, H;
 };
-// Cost of an item on the line: a step's share is the same whether one group of queries meets it or four (its bytes and the
-// instructions that every warp spends on a slice decide), and putting a result together takes as long as two steps or less.
-constexpr int kStepLog2 = 2, kItemCost = 7;
-__host__ __device__ __forceinline__ int64_t item_cost(int steps) { return ((int64_t)steps << kStepLog2) + kItemCost; }
+// Cost of an item on the line, by its queries, in units of some 750 cycles: of a step, and of putting a result together.
+// Measured with the cycle counter (head size 128, cycles of a step / of an item): bf16 caches up to 8 queries 1400 to 2300 /
+// 2000, 16 queries 1800 to 2200 / 3500, 32 queries 3500 to 4100 / 5000, 64 queries 6100 / 7000; 8-bit caches, whose steps
+// are twice as long, 2300 to 3300 / 3200, 64 queries 10500 / 9300.
+struct ItemCost {
+    int step, fixed;
+};
+template <int DT>
+__device__ __forceinline__ ItemCost item_cost(int nq) {
+    constexpr int kGroup = DT == PSMC_F32 ? 8 : 16;
+    const int c = nq <= kGroup / 2 ? 0 : (nq <= kGroup ? 1 : (nq <= 2 * kGroup ? 2 : 3));
+    if (DT == PSMC_F8) return ItemCost{c == 0 ? 4 : (c == 1 ? 6 : (c == 2 ? 10 : 14)), c == 0 ? 5 : (c == 1 ? 6 : (c == 2 ? 8 : 12))};
+    if (DT == PSMC_BF16) return ItemCost{c <= 1 ? 3 : (c == 2 ? 5 : 8), c == 0 ? 4 : (c == 1 ? 5 : (c == 2 ? 7 : 10))};
+    return ItemCost{c <= 1 ? 4 : (c == 2 ? 8 : 16), 5};
+}
+template <int DT>
 __device__ __forceinline__ int64_t seg_cost(const LineShape& s, int rows, int steps) {
-    const int qt = s.group * kGroups;
-    return (rows * s.ratio + qt - 1) / qt * item_cost(steps);
+    const int qt = s.group * kGroups, nq = rows * s.ratio, full = nq / qt, rem = nq - full * qt;
+    const ItemCost f = item_cost<DT>(qt), r = item_cost<DT>(rem);
+    return full * ((int64_t)steps * f.step + f.fixed) + (rem ? (int64_t)steps * r.step + r.fixed : 0);
 }
 __device__ __forceinline__ int steps_of(const LineShape& s, int p0, int p1) { return (p1 - p0 + s.step - 1) / s.step; }
 
@@ -70,6 +83,7 @@ constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
 constexpr int kRun = 4;              // block indices that a warp looks at in one go
 constexpr int kWarpSegs = 32;        // segments that may begin in one warp's block indices
 
+template <int DT>
 __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedView c, const PagedAttend a, const LineShape ls,
                                                                   TilePlan* plans) {
     struct Found {
@@ -202,7 +216,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
             const bool in = s < n_segs;
             const Found f = in ? segs[s] : Found{0, 0, 0};
             const int p0 = f.from * B, p1 = in ? ends[s] : 0, held = __popc(f.mask);
-            const int64_t cs = in ? seg_cost(ls, held, steps_of(ls, p0, p1)) : 0;
+            const int64_t cs = in ? seg_cost<DT>(ls, held, steps_of(ls, p0, p1)) : 0;
             const int64_t cs_upto = warp_scan_incl<long long>(cs, lane);
             const int held_upto = warp_scan_incl(held, lane);
             if (in) {
@@ -257,7 +271,7 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
     Bearings b;
     b.total = sum;
     b.share = (int64_t)__ddiv_ru((double)b.total, (double)l.workers) + 1;  // (a little more than an even share does no harm)
-    if (b.share < item_cost(1)) b.share = item_cost(1);
+    if (b.share < 9) b.share = 9;  // about an item of one step
     const int64_t x = worker * b.share;
     int64_t base = 0;
     b.tile = l.n_tiles;
@@ -278,10 +292,11 @@ __device__ __forceinline__ Bearings bearings(const Line& l, int worker, int tile
     return b;
 }
 // the steps of an item (first cost unit a) that lie before `bound`
-__device__ __forceinline__ int steps_before(int64_t bound, int64_t a, int steps) {
-    const int64_t d = bound - a - kItemCost;
+__device__ __forceinline__ int steps_before(int64_t bound, int64_t a, const ItemCost& c, int steps) {
+    const int64_t d = bound - a - c.fixed;
     if (d <= 0) return 0;
-    return (int)min((int64_t)steps, (d + (1 << kStepLog2) - 1) >> kStepLog2);
+    if (d >= (int64_t)steps * c.step) return steps;
+    return (int)(((uint32_t)d + c.step - 1) / (uint32_t)c.step);
 }
 
 // What the arithmetic of an item has to know of it; the copying side, which is ahead, leaves it in a queue.
@@ -306,6 +321,7 @@ struct Walk {
     int nq;              // queries of this query tile
     int before;          // see Segment
     int steps;
+    ItemCost cost;
     int s, s_end;        // steps of the item that are this worker's: the next one, and the end
     int s_first;
     bool done;
@@ -333,13 +349,14 @@ struct Walk {
     }
     __device__ __forceinline__ void enter_item(const Line& l, int64_t lo) {
         nq = min(kGroups * S::kGroup, __popc(mask) * l.ls.ratio - qt * kGroups * S::kGroup);
-        s_first = s = steps_before(lo, a, steps);
-        s_end = steps_before(hi, a, steps);
+        cost = item_cost<S::DT>(nq);
+        s_first = s = steps_before(lo, a, cost, steps);
+        s_end = steps_before(hi, a, cost, steps);
     }
     // the item after this one that has a step for this worker
     __device__ __forceinline__ void next_item(const Line& l) {
         do {
-            a += item_cost(steps);
+            a += (int64_t)steps * cost.step + cost.fixed;
             if (a >= hi) {
                 done = true;
                 return;
@@ -392,11 +409,11 @@ struct Walk {
             start = tp.seg[lane].start;
             head_words = *reinterpret_cast<const int2*>(&tp);
         }
-        const int64_t cost = tp.cost, x = lo - b.before;
+        const int64_t tile_cost = tp.cost, x = lo - b.before;
         n_segs = head_words.x;
         whole = (uint32_t)head_words.y;
-        head = quotient(x, cost);
-        const int64_t y = x - head * cost;
+        head = quotient(x, tile_cost);
+        const int64_t y = x - head * tile_cost;
         si = -1;
         int4 g = seg;
         int64_t first = 0;
@@ -414,9 +431,10 @@ struct Walk {
             start = tp.seg[s0 + lane].start;
         }
         enter_segment(l, g);
-        const int64_t full = item_cost(steps);
+        const ItemCost fc = item_cost<S::DT>(kGroups * S::kGroup);
+        const int64_t full = (int64_t)steps * fc.step + fc.fixed;
         qt = min(n_qt - 1, quotient(y - first, full));
-        a = b.before + head * cost + first + qt * full;
+        a = b.before + head * tile_cost + first + qt * full;
         enter_item(l, lo);
         if (s >= s_end) next_item(l);
     }
@@ -1473,6 +1491,7 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
     const Bearings b = bearings(g.l, 0, tile, lane);
     const int n_segs = tp.n_segs;
     if (tp.left_out >> in_tile & 1) return;
+    const ItemCost full = item_cost<DT>(kTileQueries);
     const int64_t line_at = b.before + head * tp.cost, tile_slots = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio);
 
     float top = -INFINITY, total = 0.f;
@@ -1488,19 +1507,21 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
         // a lane per segment: the shares k0 .. k0 + n - 1 that have, or might have, a part of this query's item
         const uint32_t mask = (uint32_t)seg.x;
         int k0 = 0, n = 0, steps = 0, in_item = 0;
+        ItemCost c{1, 0};
         int64_t a = 0, first = 0;
         if (s0 + lane < n_segs && (mask >> in_tile & 1)) {
             const int qi = __popc(mask & ((1u << in_tile) - 1)) * ls.ratio + sub, qt = qi / kTileQueries;
             in_item = qi - qt * kTileQueries;
             steps = steps_of(ls, seg.y, seg.z);
-            a = line_at + seg_start + qt * item_cost(steps);
+            a = line_at + seg_start + qt * ((int64_t)steps * full.step + full.fixed);
+            c = item_cost<DT>(min(kTileQueries, __popc(mask) * ls.ratio - qt * kTileQueries));
             first = tile_slots + (int64_t)seg.w * ls.ratio + qi;
             k0 = quotient(a, b.share);
-            n = quotient(a + item_cost(steps) - 1, b.share) - k0 + 1;
+            n = quotient(a + (int64_t)steps * c.step + c.fixed - 1, b.share) - k0 + 1;
             // in place already: the row's only segment, all of it in one share
             if (tp.whole >> in_tile & 1)
                 for (int k = k0; k < k0 + n && k < k0 + 3; ++k)
-                    if (steps_before(k * b.share, a, steps) == 0 && steps_before((k + 1) * b.share, a, steps) == steps) n = -1;
+                    if (steps_before(k * b.share, a, c, steps) == 0 && steps_before((k + 1) * b.share, a, c, steps) == steps) n = -1;
         }
         if (__any_sync(kFull, n < 0)) return;
         const int upto = warp_scan_incl(n, lane), all = __shfl_sync(kFull, upto, 31);
@@ -1514,12 +1535,13 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
             at = min(at, 31);
             const int k = __shfl_sync(kFull, k0, at) + e - (__shfl_sync(kFull, upto, at) - __shfl_sync(kFull, n, at));
             const int64_t ea = __shfl_sync(kFull, (long long)a, at), efirst = __shfl_sync(kFull, (long long)first, at);
+            const ItemCost ec{__shfl_sync(kFull, c.step, at), __shfl_sync(kFull, c.fixed, at)};
             const int esteps = __shfl_sync(kFull, steps, at), ein = __shfl_sync(kFull, in_item, at);
             int64_t slot = -1;
             float2 st = float2{-INFINITY, 0.f};
             if (e < all) {
-                const int from = steps_before(k * b.share, ea, esteps);
-                if (from < steps_before((k + 1) * b.share, ea, esteps))  // (a share may lie between two steps)
+                const int from = steps_before(k * b.share, ea, ec, esteps);
+                if (from < steps_before((k + 1) * b.share, ea, ec, esteps))  // (a share may lie between two steps)
                     slot = from == 0 ? efirst : g.l.first_rest + (int64_t)k * kTileQueries + ein;
             }
             if (slot >= 0) st = g.l.stat[slot];
@@ -1663,7 +1685,7 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.l.first_rest = sc.first_rest;
     g.l.n_tiles = sc.n_tiles;
     g.l.workers = S::kCtas * kSMs;
-    cudaError_t e = launch_chained(paged_plan_kernel, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
+    cudaError_t e = launch_chained(paged_plan_kernel<DT>, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
     if (e != cudaSuccess) return e;
     const bool tiled = c.block_len % 16 == 0;
     g.one_copy = c.D * S::kElem % kPanel == 0 ? 1 : 0;
