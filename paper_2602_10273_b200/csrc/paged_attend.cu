@@ -546,7 +546,8 @@ struct Shape {
     static constexpr int kCtas = DP <= 128 && 3 * kStage + kExtra <= kHalfSm ? 2 : 1;  // per SM (large heads need the registers)
     static constexpr int kFit = ((kCtas == 2 ? kHalfSm : kWholeSm) - kExtra) / kStage;
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
-    // a step's stage has a slot for the queries of an item that begins with it: as many as there is room for, 8 or 16
+    // A step's stage has a slot for the queries of an item that begins with it: as many as there is room for, 8 or 16.  An item
+    // of more has a stage of the ring to itself before its first step.
     static constexpr int kQueryRow = DP * 2 + 16;
     static constexpr int kLeft = (kCtas == 2 ? kHalfSm : kWholeSm) - kExtra - kStages * kStage;
     static constexpr int kSlotQueries = DT == PSMC_F32 ? 0 : (kLeft >= kStages * 16 * kQueryRow ? 16 : (kLeft >= kStages * 8 * kQueryRow ? 8 : 0));
@@ -560,7 +561,7 @@ struct AttendArgs {
     PagedView c;
     PagedAttend a;
     Line l;
-    FastDiv by_block, by_ratio, by_units, by_heads;
+    FastDiv by_block, by_ratio, by_heads;
     int q_words, q_units;  // queries start on 4-byte, 16-byte boundaries throughout
     int one_copy;        // heads are whole panels: a tiled copy brings all panels of a slice
 };
@@ -608,6 +609,7 @@ struct Feeder {
         int tile, head, row, p, p1;  // not TILED: the step itself
         bool any;        // whether there is a step at all
         int begins;      // the item that begins with it, or -1
+        int queries;     // of that item
     };
     Walk<S> walk;
     Asked first, second;
@@ -622,17 +624,28 @@ struct Feeder {
         if (walk.mask >> lane & 1) it.rows[__popc(walk.mask & ((1u << lane) - 1))] = (uint8_t)lane;
         __syncwarp();
     }
-    // an item's queries, to the slot of the stage that its first step goes to
-    __device__ __forceinline__ void copy_queries(const AttendArgs& g, const Item& it, char* slot) {
-        const int units = g.c.D / 8;
+    // an item's queries, with zeros behind the head
+    __device__ __forceinline__ void copy_queries(const AttendArgs& g, const Item& it, char* to) {
+        constexpr int kUnits = S::DP / 8;
         const ItemHead& h = it.head_part;
-        for (int x = lane; x < h.nq * units; x += 32) {
-            const int in_tile = div_by(x, g.by_units), u = x - in_tile * units;
+        for (int x = lane; x < h.nq * kUnits; x += 32) {
+            const int in_tile = x / kUnits, u = x - in_tile * kUnits;
             int row, qh;
             place<S>(g, h, it.rows, in_tile, &row, &qh);
             const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(g.a.q.data) + (int64_t)row * g.a.q.stride_row + (int64_t)qh * g.a.q.stride_head;
-            copy16(smem_of(slot + in_tile * S::kQueryRow + u * 16), q + u * 8, 16);
+            const bool in = u * 8 < g.c.D;
+            copy16(smem_of(to + in_tile * S::kQueryRow + u * 16), q + (in ? u * 8 : 0), in ? 16 : 0);
         }
+    }
+    // a stage that holds nothing but the queries of the item that begins with the step asked for first
+    __device__ __forceinline__ void issue_queries(const AttendArgs& g, int to, char* ring, Shared<S>& sh) {
+        if (which == 0) {
+            if (lane == 0) sh.valid[to][0] = 0;
+            copy_queries(g, sh.queue[first.begins % kQueue], ring + to * S::kStage);
+        }
+        if (lane_arrivals(which)) copies_arrive(&sh.full[to]);
+        __syncwarp();
+        if (lane == 0) mbar_expect_tx(&sh.full[to], 0);
     }
     __device__ __forceinline__ Asked ask(const AttendArgs& g, Shared<S>& sh) {
         Asked q{};
@@ -641,6 +654,7 @@ struct Feeder {
         if (!walk.done) {
             if (walk.s == walk.s_first) {
                 q.begins = items;
+                q.queries = walk.nq;
                 if (which == 0) open_item(sh, g);
                 ++items;
             }
@@ -670,12 +684,8 @@ struct Feeder {
         char* stage = ring + to * S::kStage + which * S::kHalf;
         uint8_t* scales = reinterpret_cast<uint8_t*>(ring) + to * S::kStage + 2 * S::kHalf + which * S::kScales;
         const char* pool = which ? g.c.v : g.c.k;
-        if (S::kSlots > 0 && which == 0) {
-            if (first.begins >= 0 && g.q_units) {
-                const Item& it = sh.queue[first.begins % kQueue];
-                if (it.head_part.nq <= S::kSlotQueries) copy_queries(g, it, ring + S::kStages * S::kStage + to * S::kSlots);
-            }
-        }
+        if (S::kSlots > 0 && which == 0 && first.begins >= 0 && g.q_units && first.queries <= S::kSlotQueries)
+            copy_queries(g, sh.queue[first.begins % kQueue], ring + S::kStages * S::kStage + to * S::kSlots);
         if (TILED) {
             copies_wait<1>();  // the entries asked for last may still be on their way
             const int entry = first.live > 0 ? sh.entries[which][(asked - 2) % 4][lane] : -1;
@@ -746,11 +756,19 @@ struct Feeder {
         second = ask(g, sh);
         int stage = 0;
         uint32_t phase = 1;  // (a barrier that nothing has happened to yet lets the phase before its first pass)
-        for (;;) {
-            if (!mbar_wait(&sh.empty[stage], phase)) {
-                if (lane == 0) raise_status(g.a.status, PSMC_E_TIMEOUT);
-                return;
+        const auto free_stage = [&]() -> bool {
+            if (mbar_wait(&sh.empty[stage], phase)) return true;
+            if (lane == 0) raise_status(g.a.status, PSMC_E_TIMEOUT);
+            return false;
+        };
+        const auto next_stage = [&] {
+            if (++stage == S::kStages) {
+                stage = 0;
+                phase ^= 1u;
             }
+        };
+        for (;;) {
+            if (!free_stage()) return;
             if (!first.any) {
                 if (lane == 0) {
                     if (which == 0) sh.valid[stage][0] = kEnd;
@@ -759,11 +777,13 @@ struct Feeder {
                 if (lane_arrivals(which)) copies_arrive(&sh.full[stage]);
                 return;
             }
-            issue(g, stage, ring, sh);
-            if (++stage == S::kStages) {
-                stage = 0;
-                phase ^= 1u;
+            if (S::kSlots > 0 && first.begins >= 0 && g.q_units && first.queries > S::kSlotQueries) {
+                issue_queries(g, stage, ring, sh);
+                next_stage();
+                if (!free_stage()) return;
             }
+            issue(g, stage, ring, sh);
+            next_stage();
         }
     }
 };
@@ -1166,10 +1186,17 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S
     const bool busy = dv.slice < dv.slices && dv.group * S::kGroup < it.nq;
     bool fine = true;
     RawQueries<S, NT> q;
-    if (S::kSlots > 0 && g.q_units && it.nq <= S::kSlotQueries)
-        fetch_queries<S, NT>(smem_of(pp.ring + S::kStages * S::kStage + pp.stage * S::kSlots) + dv.group * S::kGroup * S::kQueryRow, q, lane);
-    else
+    if (S::kSlots > 0 && g.q_units) {  // in the slot of the first step's stage, or in a stage before it
+        const bool slot = it.nq <= S::kSlotQueries;
+        const char* at = slot ? pp.ring + S::kStages * S::kStage + pp.stage * S::kSlots : pp.ring + pp.stage * S::kStage;
+        fetch_queries<S, NT>(smem_of(at) + dv.group * S::kGroup * S::kQueryRow, q, lane);
+        if (!slot) {
+            release<S>(sh, pp.stage, lane);
+            next_stage<S>(pp);
+        }
+    } else {
         load_queries<S, NT>(g, it, rows, q, pp);
+    }
     Ti ti;
     ti.clear(q, g.a.scale * kLog2e, lane);
     int used = pp.stage;  // the stage worked on last: kept until the result is written, which passes through it
@@ -1256,9 +1283,6 @@ __device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe&
     pp.lane = threadIdx.x & 31;
     pp.warp = threadIdx.x >> 5;
     pp.worker = blockIdx.x;
-    if (S::kSlots > 0 && g.c.D < S::DP)  // components beyond the head: never copied, always zero
-        for (int i = threadIdx.x; i < S::kStages * S::kSlots / 16; i += kThreads)
-            reinterpret_cast<uint4*>(pp.ring + S::kStages * S::kStage)[i] = uint4{0, 0, 0, 0};
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&sh.full[i], (Feeder<S, TILED>::lane_arrivals(0) ? 33 : 1) + (Feeder<S, TILED>::lane_arrivals(1) ? 33 : 1));
@@ -1675,8 +1699,7 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.l.ls = LineShape{S::kStep, S::kGroup, a.Hq / c.H, c.H};
     g.by_ratio = fast_div(g.l.ls.ratio);
     g.by_heads = fast_div(a.Hq);
-    g.by_units = fast_div(c.D < 8 ? 1 : c.D / 8);
-    g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
+g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
     g.q_units = ((uint64_t)(uintptr_t)a.q.data % 16 == 0 && a.q.stride_row % 8 == 0 && a.q.stride_head % 8 == 0 && c.D % 8 == 0) ? 1 : 0;
     TilePlan* plans = reinterpret_cast<TilePlan*>(scratch + sc.plans);
     g.l.plans = plans;
