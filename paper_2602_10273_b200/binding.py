@@ -10,6 +10,8 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import struct
+import threading
 
 import numpy as np
 import torch
@@ -398,10 +400,10 @@ class Psmc:
         else:
             _check_ints(rows, n, dev)
             _check_ints(positions, n, dev)
-        heads, q_out = _write_heads(k, v, q, q_out, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, stream)
-        at = C.addressof(heads)
-        _launch(dev, "psmc_kv_paged_write", self._h, C.byref(pools), layer, n, _ptr(rows), _ptr(positions), _ref(rope), at, at + 24,
-                0 if q is None else q.shape[1], 0 if q is None else at + 48, 0 if q is None else at + 72, _raw_stream(stream, dev))
+        q_out, Hq = _write_heads(k, v, q, q_out, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, stream)
+        at = _heads.at
+        _launch(dev, lib().psmc_kv_paged_write, self._h, C.byref(pools), layer, n, _ptr(rows), _ptr(positions), _ref(rope), at, at + 24,
+                Hq, at + 48 if Hq else 0, at + 72 if Hq else 0, _raw_stream(stream, dev))
         return q_out
 
     def kv_paged_attend(self, pools: KvPools, layer: int, q: torch.Tensor, scale: float, out: torch.Tensor = None,
@@ -409,11 +411,11 @@ class Psmc:
         """psmc_kv_paged_attend: q [R, Hq, D] of every row's new token over its len + 1 positions (finished rows of out and
         lse are left as they were; zeros in an out allocated here)."""
         dev = q.get_device()
-        heads, out = _attend_heads(q, out, lse, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, True, stream)
         need = lib().psmc_paged_attend_scratch_bytes(self.R, q.shape[1], pools.n_kv_heads, pools.head_dim)
         scratch = _scratch(scratch, need, dev, stream)
-        at = C.addressof(heads)
-        _launch(dev, "psmc_kv_paged_attend", self._h, C.byref(pools), layer, q.shape[1], at, at + 24, scale, _ptr(lse),
+        out = _attend_heads(q, out, lse, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, True, stream)
+        at = _heads.at
+        _launch(dev, lib().psmc_kv_paged_attend, self._h, C.byref(pools), layer, q.shape[1], at, at + 24, scale, _ptr(lse),
                 scratch.data_ptr(), scratch.numel(), _raw_stream(stream, dev))
         return out
 
@@ -422,7 +424,7 @@ class Psmc:
         d = k_out if k_out is not None else v_out
         dev = d.get_device()
         _check_dense(k_out, v_out, d, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev)
-        _launch(dev, "psmc_kv_paged_read", self._h, C.byref(pools), layer, _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0),
+        _launch(dev, lib().psmc_kv_paged_read, self._h, C.byref(pools), layer, _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0),
                 d.stride(1), _raw_stream(stream, dev))
 
     def reindex_kv_paged(self, pools: KvPools, stream=None):
@@ -548,23 +550,33 @@ class PagedKv(PagedKvDesc):
         super().__init__(k.data_ptr(), v.data_ptr(), table.data_ptr(), table.stride(0), table.shape[0], k.shape[0], block_len,
                          table.shape[1], n_kv_heads, head_dim, dt)
         self._keep = (k, v, table)
-        self.index, self.io = k.get_device(), _io_dtype(dt)
+        self.index, self.io, self.address = k.get_device(), _io_dtype(dt), C.addressof(self)
+        self.rows, self.heads, self.dim = table.shape[0], n_kv_heads, head_dim  # (fields of a C structure take longer to read)
 
 
 # A decode loop makes two of these calls per layer and token, on small tensors: what happens on the host is kept short.
-_HeadsArray = C.c_int64 * 12  # up to four psmc_heads: {address, row stride, head stride}
+class _Heads(threading.local):
+    """Up to four psmc_heads {address, row stride, head stride} of the call that this thread is making (the library has read
+    them when the call returns)."""
+
+    def __init__(self):
+        self.buffer = (C.c_int64 * 12)()
+        self.at = C.addressof(self.buffer)
 
 
-def _launch(index: int, name: str, *args) -> None:
+_heads = _Heads()
+_pack_heads = struct.Struct("12q").pack_into
+
+
+def _launch(index: int, fn, *args) -> None:
     """Calls the library with the tensors' device current, whichever is."""
-    fn = getattr(lib(), name)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         code = fn(*args)
     else:
         with torch.cuda.device(index):
             code = fn(*args)
     if code != OK:
-        raise PsmcError(code, name)
+        raise PsmcError(code, fn.__name__)
 
 
 def _raw_stream(stream, index: int) -> int:
@@ -589,38 +601,45 @@ def _io_dtype(dtype_code: int):
 
 
 def _check_heads(t, shape, io, index):
-    assert t.shape == shape and t.dtype is io and t.get_device() == index and t.stride(2) == 1
+    """Checks a [n, heads, head_dim] tensor; its strides."""
+    strides = t.stride()
+    assert t.shape == shape and t.dtype is io and t.get_device() == index and strides[2] == 1
+    return strides
 
 
 def _write_heads(k, v, q, q_out, H, D, io, index, stream):
+    """Checks the tensors of a write and leaves them in _heads.buffer; q_out, and how many query heads there are."""
     assert index >= 0
     n = k.shape[0]
-    _check_heads(k, (n, H, D), io, index)
-    _check_heads(v, (n, H, D), io, index)
+    shape = (n, H, D)
+    ks, vs = _check_heads(k, shape, io, index), _check_heads(v, shape, io, index)
     if q is None:
         assert q_out is None
-        return _HeadsArray(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1)), None
+        _pack_heads(_heads.buffer, 0, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], 0, 0, 0, 0, 0, 0)
+        return None, 0
     if q_out is None:
         with _allocate_on(stream):
             q_out = torch.empty_like(q)
-    shape = (n, q.shape[1], D)
-    _check_heads(q, shape, io, index)
-    _check_heads(q_out, shape, io, index)
-    return _HeadsArray(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), q.data_ptr(), q.stride(0),
-                       q.stride(1), q_out.data_ptr(), q_out.stride(0), q_out.stride(1)), q_out
+    Hq = q.shape[1]
+    shape = (n, Hq, D)
+    qs, os_ = _check_heads(q, shape, io, index), _check_heads(q_out, shape, io, index)
+    _pack_heads(_heads.buffer, 0, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], q.data_ptr(), qs[0], qs[1], q_out.data_ptr(),
+                os_[0], os_[1])
+    return q_out, Hq
 
 
 def _attend_heads(q, out, lse, R, H, D, io, index, zeros, stream):
     assert index >= 0 and q.dim() == 3 and q.shape[1] % H == 0
     shape = (R, q.shape[1], D)
-    _check_heads(q, shape, io, index)
+    qs = _check_heads(q, shape, io, index)
     if out is None:
         with _allocate_on(stream):
             out = torch.zeros_like(q) if zeros else torch.empty_like(q)
-    _check_heads(out, shape, io, index)
+    os_ = _check_heads(out, shape, io, index)
     if lse is not None:
         assert lse.get_device() == index and lse.dtype is torch.float32 and lse.is_contiguous() and lse.shape == shape[:2]
-    return _HeadsArray(q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1)), out
+    _pack_heads(_heads.buffer, 0, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1], 0, 0, 0, 0, 0, 0)
+    return out
 
 
 def _check_ints(t, n, index):
@@ -636,10 +655,11 @@ def _check_optional(skip, status_word, R, index):
 
 def _check_dense(k_out, v_out, d, R, H, D, io, index):
     assert index >= 0
+    shape, strides = d.shape, d.stride()
     for t in (k_out, v_out):
         if t is not None:
-            assert t.get_device() == index and t.dtype is io and t.shape == d.shape and t.stride() == d.stride()
-    assert d.dim() == 4 and d.shape[0] == R and d.shape[1] == H and d.shape[3] == D and d.stride(3) == 1 and d.stride(2) == D
+            assert t.get_device() == index and t.dtype is io and t.shape == shape and t.stride() == strides
+    assert len(shape) == 4 and shape[0] == R and shape[1] == H and shape[3] == D and strides[3] == 1 and strides[2] == D
 
 
 def _scratch(scratch, need, index, stream):
@@ -660,12 +680,13 @@ def paged_write(cache: PagedKv, k: torch.Tensor, v: torch.Tensor, rows, position
     if rows is not None:
         _check_ints(rows, n, dev)
     _check_ints(positions, n, dev)
-    _check_optional(skip, status_word, cache.R, dev)
-    heads, q_out = _write_heads(k, v, q, q_out, cache.n_kv_heads, cache.head_dim, cache.io, dev, stream)
-    at = C.addressof(heads)
-    _launch(dev, "psmc_paged_write", C.addressof(cache), n, _ptr(rows), positions.data_ptr(), _ptr(skip), _ref(rope), at, at + 24,
-            0 if q is None else q.shape[1], 0 if q is None else at + 48, 0 if q is None else at + 72, _ptr(status_word),
-            _raw_stream(stream, dev))
+    if skip is not None or status_word is not None:
+        _check_optional(skip, status_word, cache.rows, dev)
+    q_out, Hq = _write_heads(k, v, q, q_out, cache.heads, cache.dim, cache.io, dev, stream)
+    at = _heads.at
+    _launch(dev, lib().psmc_paged_write, cache.address, n, 0 if rows is None else rows.data_ptr(), positions.data_ptr(),
+            0 if skip is None else skip.data_ptr(), _ref(rope), at, at + 24, Hq, at + 48 if Hq else 0, at + 72 if Hq else 0,
+            0 if status_word is None else status_word.data_ptr(), _raw_stream(stream, dev))
     return q_out
 
 
@@ -674,15 +695,17 @@ def paged_attend(cache: PagedKv, q: torch.Tensor, lens: torch.Tensor, scale: flo
                  status_word: torch.Tensor = None, stream=None) -> torch.Tensor:
     """psmc_paged_attend: q [R, Hq, D], one token per row, over positions 0 .. lens[r] + extra of the row (lens int32 [R]).
     lse: float32 [R, Hq] or None.  Rows with skip != 0 are left as they were (zeros in an out allocated here)."""
-    dev, R, H, D = cache.index, cache.R, cache.n_kv_heads, cache.head_dim
+    dev, R, H, D, L = cache.index, cache.rows, cache.heads, cache.dim, lib()
     _check_ints(lens, R, dev)
-    _check_optional(skip, status_word, R, dev)
-    heads, out = _attend_heads(q, out, lse, R, H, D, cache.io, dev, skip is not None, stream)
+    if skip is not None or status_word is not None:
+        _check_optional(skip, status_word, R, dev)
     Hq = q.shape[1]
-    scratch = _scratch(scratch, lib().psmc_paged_attend_scratch_bytes(R, Hq, H, D), dev, stream)
-    at = C.addressof(heads)
-    _launch(dev, "psmc_paged_attend", C.addressof(cache), lens.data_ptr(), extra, _ptr(skip), Hq, at, at + 24, scale, _ptr(lse),
-            scratch.data_ptr(), scratch.numel(), _ptr(status_word), _raw_stream(stream, dev))
+    scratch = _scratch(scratch, L.psmc_paged_attend_scratch_bytes(R, Hq, H, D), dev, stream)
+    out = _attend_heads(q, out, lse, R, H, D, cache.io, dev, skip is not None, stream)
+    at = _heads.at
+    _launch(dev, L.psmc_paged_attend, cache.address, lens.data_ptr(), extra, 0 if skip is None else skip.data_ptr(), Hq, at, at + 24,
+            scale, 0 if lse is None else lse.data_ptr(), scratch.data_ptr(), scratch.numel(),
+            0 if status_word is None else status_word.data_ptr(), _raw_stream(stream, dev))
     return out
 
 
@@ -691,11 +714,13 @@ def paged_read(cache: PagedKv, lens: torch.Tensor, k_out: torch.Tensor = None, v
     """psmc_paged_read: positions 0 .. lens[r] of every row into dense [R, H, max_len, D] tensors (one of them may be None)."""
     dev = cache.index
     d = k_out if k_out is not None else v_out
-    _check_dense(k_out, v_out, d, cache.R, cache.n_kv_heads, cache.head_dim, cache.io, dev)
-    _check_ints(lens, cache.R, dev)
-    _check_optional(skip, status_word, cache.R, dev)
-    _launch(dev, "psmc_paged_read", C.addressof(cache), lens.data_ptr(), _ptr(skip), _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0),
-            d.stride(1), _ptr(status_word), _raw_stream(stream, dev))
+    _check_dense(k_out, v_out, d, cache.rows, cache.heads, cache.dim, cache.io, dev)
+    _check_ints(lens, cache.rows, dev)
+    if skip is not None or status_word is not None:
+        _check_optional(skip, status_word, cache.rows, dev)
+    strides = d.stride()
+    _launch(dev, lib().psmc_paged_read, cache.address, lens.data_ptr(), 0 if skip is None else skip.data_ptr(), _ptr(k_out), _ptr(v_out),
+            d.shape[2], strides[0], strides[1], 0 if status_word is None else status_word.data_ptr(), _raw_stream(stream, dev))
 
 
 def logits_pass_scratch_bytes(R: int, V: int) -> int:

@@ -15,6 +15,8 @@
 //           warp, and where that leaves warps over, by positions.
 //   join    per (row, query head): the partial results of the row's segments and of the shares that split them.
 //
+// Few rows of short capacity take the middle kernel alone, a CTA for each (row, key-value head): see launch().
+//
 // Scores and outputs are formed transposed, S^T = K Q^T and O^T = V^T P^T, on the warp-level matrix instructions: the 16
 // rows of an operand tile are positions (or components of the output) and its 8 columns queries, so that the 4 to 8
 // queries of one key-value head fill a tile, and K and V come straight from their rows in shared memory.  (These
@@ -245,6 +247,7 @@ struct Line {
     float* part;         // [.., D] unnormalised outputs: those of whole items and first parts, then one set per worker
     float2* stat;        // {reference, sum} of each
     int64_t first_rest;  // where the sets of the workers begin
+    int direct;          // no plan: worker i has (row, head, query tile) number i, all of it
     LineShape ls;
 };
 
@@ -355,6 +358,10 @@ struct Walk {
     }
     // the item after this one that has a step for this worker
     __device__ __forceinline__ void next_item(const Line& l) {
+        if (l.direct) {
+            done = true;
+            return;
+        }
         do {
             a += (int64_t)steps * cost.step + cost.fixed;
             if (a >= hi) {
@@ -437,6 +444,18 @@ struct Walk {
         a = b.before + head * tile_cost + first + qt * full;
         enter_item(l, lo);
         if (s >= s_end) next_item(l);
+    }
+    // l.direct: n positions of the row (what the plan would have found out)
+    __device__ __forceinline__ void begin_direct(const Line& l, int row, int head_, int qt_, int n) {
+        tile = row / kTileRows;
+        mask = whole = 1u << (row % kTileRows);
+        head = head_;
+        qt = qt_;
+        p0 = before = s = s_first = 0;
+        p1 = n;
+        steps = s_end = (n + S::kStep - 1) / S::kStep;
+        nq = min(kGroups * S::kGroup, l.ls.ratio - qt * kGroups * S::kGroup);
+        done = steps == 0;
     }
     __device__ __forceinline__ ItemHead item(const Line& l, int worker) const {
         ItemHead it;
@@ -746,12 +765,34 @@ struct Feeder {
         first = second;
         second = ask(g, sh);
     }
+    __device__ __forceinline__ void begin_direct(const AttendArgs& g) {
+        using T = typename PoolIo<S::DT>::type;
+        const int tiles = (g.l.ls.ratio + kGroups * S::kGroup - 1) / (kGroups * S::kGroup), per_row = g.c.H * tiles;
+        const int row = worker / per_row, x = worker - row * per_row, head = x / tiles, qt = x - head * tiles;
+        walk.done = true;
+        if (g.a.skip && g.a.skip[row]) return;
+        const int64_t room = (int64_t)g.c.max_blocks * g.c.block_len;
+        int64_t n = (int64_t)__ldg(g.a.lens + row) + g.a.extra;
+        if (n > room) {
+            if (lane == 0) raise_status(g.a.status, PSMC_E_STATE);
+            n = room;
+        }
+        walk.begin_direct(g.l, row, head, qt, (int)max((int64_t)0, n));
+        if (!walk.done || which != 0) return;
+        for (int q = 0; q < walk.nq; ++q) {  // no positions: zeros
+            const int qh = head * g.l.ls.ratio + qt * kGroups * S::kGroup + q;
+            T* out = static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head;
+            for (int d = lane; d < g.c.D; d += 32) out[d] = from_float<T>(0.f);
+            if (lane == 0 && g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = -INFINITY;
+        }
+    }
     __device__ __forceinline__ void run(const AttendArgs& g, char* ring, Shared<S>& sh) {
         lane = threadIdx.x & 31;
         worker = blockIdx.x;
         which = (threadIdx.x >> 5) - kWarps;
         items = asked = 0;
-        walk.begin(g.l, worker, lane);
+        if (g.l.direct) begin_direct(g);
+        else walk.begin(g.l, worker, lane);
         first = ask(g, sh);
         second = ask(g, sh);
         int stage = 0;
@@ -1708,7 +1749,14 @@ g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 &
     g.l.first_rest = sc.first_rest;
     g.l.n_tiles = sc.n_tiles;
     g.l.workers = S::kCtas * kSMs;
-    cudaError_t e = launch_chained(paged_plan_kernel<DT>, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
+    // A grid of one CTA per (row, key-value head, query tile) that fits the GPU at once, over rows of at most 16 steps: what
+    // splitting and sharing would save is less than the two other kernels cost (4 fp32 rows of 121 positions 17 -> 8 us, 8 rows
+    // of 1000 positions with 32 heads each 23 -> 17 us; the results do not depend on the lengths at hand, which only the device
+    // knows, but on the room that the table has).
+    const int64_t direct = (int64_t)c.R * c.H * ((g.l.ls.ratio + kGroups * S::kGroup - 1) / (kGroups * S::kGroup));
+    g.l.direct = direct <= g.l.workers && (int64_t)c.max_blocks * c.block_len <= 16 * S::kStep ? 1 : 0;
+    if (g.l.direct) g.l.workers = (int)direct;
+    cudaError_t e = g.l.direct ? cudaSuccess : launch_chained(paged_plan_kernel<DT>, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
     if (e != cudaSuccess) return e;
     const bool tiled = c.block_len % 16 == 0;
     g.one_copy = c.D * S::kElem % kPanel == 0 ? 1 : 0;
@@ -1718,7 +1766,7 @@ g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 &
     else fn = tiled ? paged_attend_kernel<S, true> : paged_attend_kernel<S, false>;
     e = allow_dynamic_smem(reinterpret_cast<const void*>(fn), S::kBytes);
     if (e == cudaSuccess) e = launch_chained(fn, dim3((unsigned)g.l.workers), dim3(kThreads), S::kBytes, stream, g);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || g.l.direct) return e;
     // few queries: four warps each, for what may be many partial results of a long row
     const int64_t queries = (int64_t)c.R * a.Hq;
     constexpr int kOwn = DP > 128 ? 2 : 1;

@@ -126,9 +126,11 @@ SHAPES = [  # dt, H, queries per key-value head, D, page, lens, share
 ]
 
 
+@pytest.mark.parametrize("room", ["tight", "wide"])
 @pytest.mark.parametrize("dt,H,ratio,D,page,lens,share", SHAPES, ids=lambda v: str(v)[:24].replace(" ", ""))
-def test_attend(dt, H, ratio, D, page, lens, share):
-    c = Cache(dt, lens, H, D, page, seed=5, share=share, spare_cols=3)
+def test_attend(dt, H, ratio, D, page, lens, share, room):
+    """room: a table hardly wider than the rows need, or one wide enough for the split form whatever the lengths."""
+    c = Cache(dt, lens, H, D, page, seed=5, share=share, spare_cols=3 if room == "tight" else 3 + 2048 // page)
     g = torch.Generator(device="cuda").manual_seed(9)
     q = (1.5 * torch.randn((c.R, H * ratio, D), device="cuda", generator=g)).to(IO[dt])
     lse = torch.full((c.R, H * ratio), 7.0, device="cuda")
