@@ -552,7 +552,6 @@ struct Shape {
     static constexpr int kStep = DT == PSMC_F32 && DP > 128 ? 32 : (DT == PSMC_F8 && DP <= 128 ? 128 : 64);  // positions
     static constexpr int kSlices = kStep / 16;                            // the 16 positions of an operand tile
     static constexpr int kSlice = kPanelOfSlice * kPanels;                // bytes of one, of keys or values
-    static constexpr int kPair = kSlices > kWarps ? 2 : 1;                // slices that a warp takes at a time
     static constexpr int kHalf = kStep * kPanel * kPanels;                // keys, then values
     static constexpr int kScales = DT == PSMC_F8 ? kStep : 0;             // scale bytes
     static constexpr int kStage = (2 * (kHalf + kScales) + 1023) / 1024 * 1024;
@@ -968,82 +967,69 @@ struct Tiles {
         }
     }
 
-    // MT slices: keys[m], vals[m]: shared addresses of their 16 rows; valid[m]: which of them hold something; k_scale[m],
-    // v_byte[m]: lane p's scales (8-bit)
-    template <int MT>
-    __device__ __forceinline__ void step(const RawQueries<S, NT>& q, const uint32_t (&keys)[MT], const uint32_t (&vals)[MT], const uint32_t (&valid)[MT],
-                                         const float (&k_scale)[MT], const int (&v_byte)[MT], int lane) {
+    // One slice.  keys, vals: shared addresses of its 16 rows; valid: which of them hold something; k_scale, v_byte: lane p's
+    // scales (8-bit).  (Two slices at a time, for longer chains of independent work, measured the same.)
+    __device__ __forceinline__ void step(const RawQueries<S, NT>& q, uint32_t keys, uint32_t vals, uint32_t valid, float k_scale, int v_byte,
+                                         int lane) {
         const int gq = lane >> 2;
-        float s[MT][NT][4], s2[MT][NT][4];  // two chains, so that the products of one tile wait less for each other
+        float s[NT][4], s2[NT][4];  // two chains, so that the products of one tile wait less for each other
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[m][j][e] = s2[m][j][e] = 0.f;
+            for (int e = 0; e < 4; ++e) s[j][e] = s2[j][e] = 0.f;
         // unit u of a row lies at u ^ (row % 8); the lane's row, and its unit before the exchange within a pair
-        const uint32_t krow = (lane & 15) * kPanel, kunit = ((lane >> 4) ^ (lane & 7)) << 4;
+        const uint32_t krow = keys + (lane & 15) * kPanel, kunit = ((lane >> 4) ^ (lane & 7)) << 4;
         if (!kF8) {
 #pragma unroll
-            for (int ks = 0; ks < kDt; ++ks)
+            for (int ks = 0; ks < kDt; ++ks) {
+                uint32_t ka[4];
+                load_tiles(ka, krow + (2 * ks / 8) * kPanelOfSlice + ((2 * ks % 8 << 4) ^ kunit));
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    uint32_t ka[4];
-                    load_tiles(ka, keys[m] + krow + (2 * ks / 8) * kPanelOfSlice + ((2 * ks % 8 << 4) ^ kunit));
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) mma<false>(ks & 1 ? s2[m][j] : s[m][j], ka, q.x[j][ks][0], q.x[j][ks][1]);
-                }
+                for (int j = 0; j < NT; ++j) mma<false>(ks & 1 ? s2[j] : s[j], ka, q.x[j][ks][0], q.x[j][ks][1]);
+            }
         } else {
 #pragma unroll
-            for (int ks = 0; ks < kDt; ks += 2)  // 32 components: two tiles of 16
+            for (int ks = 0; ks < kDt; ks += 2) {  // 32 components: two tiles of 16
+                uint32_t kc[4];
+                load_tiles(kc, krow + (ks / 8) * kPanelOfSlice + ((ks % 8 << 4) ^ kunit));
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    uint32_t kc[4];
-                    load_tiles(kc, keys[m] + krow + (ks / 8) * kPanelOfSlice + ((ks % 8 << 4) ^ kunit));
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t ka[4] = {codes_to_f16(kc[2 * u]), codes_to_f16(kc[2 * u + 1]), codes_to_f16(kc[2 * u] >> 16),
+                                            codes_to_f16(kc[2 * u + 1] >> 16)};
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t ka[4] = {codes_to_f16(kc[2 * u]), codes_to_f16(kc[2 * u + 1]), codes_to_f16(kc[2 * u] >> 16),
-                                                codes_to_f16(kc[2 * u + 1] >> 16)};
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) mma<true>(u ? s2[m][j] : s[m][j], ka, q.x[j][ks + u][0], q.x[j][ks + u][1]);
-                    }
+                    for (int j = 0; j < NT; ++j) mma<true>(u ? s2[j] : s[j], ka, q.x[j][ks + u][0], q.x[j][ks + u][1]);
                 }
+            }
         }
         // scaled to log2 units; positions without anything get -inf
-        float iv[MT][2];
+        const bool ok0 = valid >> gq & 1, ok1 = valid >> (gq + 8) & 1;
+        float ev0 = 0.f, ev1 = 0.f, ks0 = 1.f, ks1 = 1.f, iv0 = 0.f, iv1 = 0.f;  // 8-bit: scales of positions gq, gq + 8
+        if (kF8) {
+            ks0 = __shfl_sync(kFull, k_scale, gq);
+            ks1 = __shfl_sync(kFull, k_scale, gq + 8);
+            const int b0 = __shfl_sync(kFull, v_byte, gq), b1 = __shfl_sync(kFull, v_byte, gq + 8);
+            ev0 = (float)(b0 - 127);
+            ev1 = (float)(b1 - 127);
+            iv0 = ok0 ? __uint_as_float((uint32_t)(254 - b0) << 23) : 0.f;
+            iv1 = ok1 ? __uint_as_float((uint32_t)(254 - b1) << 23) : 0.f;
+        }
         bool grow = false;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const bool ok0 = valid[m] >> gq & 1, ok1 = valid[m] >> (gq + 8) & 1;
-            float ev0 = 0.f, ev1 = 0.f, ks0 = 1.f, ks1 = 1.f;  // 8-bit: scales of positions gq, gq + 8
-            if (kF8) {
-                ks0 = __shfl_sync(kFull, k_scale[m], gq);
-                ks1 = __shfl_sync(kFull, k_scale[m], gq + 8);
-                const int b0 = __shfl_sync(kFull, v_byte[m], gq), b1 = __shfl_sync(kFull, v_byte[m], gq + 8);
-                ev0 = (float)(b0 - 127);
-                ev1 = (float)(b1 - 127);
-                iv[m][0] = ok0 ? __uint_as_float((uint32_t)(254 - b0) << 23) : 0.f;
-                iv[m][1] = ok1 ? __uint_as_float((uint32_t)(254 - b1) << 23) : 0.f;
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = (s[j][e] + s2[j][e]) * sc[j][e & 1];
+                if (kF8) x = fmaf(x, e < 2 ? ks0 : ks1, e < 2 ? ev0 : ev1);
+                x = (e < 2 ? ok0 : ok1) ? x : -INFINITY;
+                s[j][e] = x;
+                grow = grow || x > ref[j][e & 1] + kSlack;
             }
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = (s[m][j][e] + s2[m][j][e]) * sc[j][e & 1];
-                    if (kF8) x = fmaf(x, e < 2 ? ks0 : ks1, e < 2 ? ev0 : ev1);
-                    x = (e < 2 ? ok0 : ok1) ? x : -INFINITY;
-                    s[m][j][e] = x;
-                    grow = grow || x > ref[j][e & 1] + kSlack;
-                }
-        }
         if (__any_sync(kFull, grow)) {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float top = ref[j][i];
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) top = fmaxf(top, fmaxf(s[m][j][i], s[m][j][i + 2]));
+                    float top = fmaxf(ref[j][i], fmaxf(s[j][i], s[j][i + 2]));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
@@ -1060,64 +1046,58 @@ struct Tiles {
                 }
         }
         // weights, as the second operand of O^T += V^T P^T: [positions, queries], turned 8 x 8 at a time
-        uint32_t p[MT][NT][kF8 ? 1 : 2][2];
+        uint32_t p[NT][kF8 ? 1 : 2][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const float r0 = ref[j][0] == -INFINITY ? 0.f : ref[j][0], r1 = ref[j][1] == -INFINITY ? 0.f : ref[j][1];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float p0 = ex2(s[m][j][2 * h] - r0), p1 = ex2(s[m][j][2 * h + 1] - r1);
-                    if (kF8) {
-                        // weights of the codes: the values' scale is in the exponent already, and the sum takes it out again;
-                        // fp16 holds 11 bits of a weight down to 2^-14 of the largest
-                        sum[j][0] = fmaf(p0, iv[m][h], sum[j][0]);
-                        sum[j][1] = fmaf(p1, iv[m][h], sum[j][1]);
-                        p[m][j][0][h] = turn_tile(pack_f16(p0, p1));
-                    } else {
-                        // a weight as the sum of two bf16 numbers: 16 bits of it instead of 8
-                        sum[j][0] += p0;
-                        sum[j][1] += p1;
-                        const uint32_t hi = pack_bf16(p0, p1);
-                        p[m][j][0][h] = turn_tile(hi);
-                        p[m][j][kF8 ? 0 : 1][h] = turn_tile(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
-                    }
+            for (int h = 0; h < 2; ++h) {
+                const float p0 = ex2(s[j][2 * h] - r0), p1 = ex2(s[j][2 * h + 1] - r1);
+                if (kF8) {
+                    // weights of the codes: the values' scale is in the exponent already, and the sum takes it out again; fp16
+                    // holds 11 bits of a weight down to 2^-14 of the largest
+                    sum[j][0] = fmaf(p0, h ? iv1 : iv0, sum[j][0]);
+                    sum[j][1] = fmaf(p1, h ? iv1 : iv0, sum[j][1]);
+                    p[j][0][h] = turn_tile(pack_f16(p0, p1));
+                } else {
+                    // a weight as the sum of two bf16 numbers: 16 bits of it instead of 8
+                    sum[j][0] += p0;
+                    sum[j][1] += p1;
+                    const uint32_t hi = pack_bf16(p0, p1);
+                    p[j][0][h] = turn_tile(hi);
+                    p[j][kF8 ? 0 : 1][h] = turn_tile(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
                 }
+            }
         }
-        const uint32_t vrow = ((lane & 7) + (lane >> 4) * 8) * kPanel, vunit = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
+        const uint32_t vrow = vals + ((lane & 7) + (lane >> 4) * 8) * kPanel, vunit = ((lane >> 3 & 1) ^ (lane & 7)) << 4;
         if (!kF8) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int d = 0; d < kDt; ++d) {
+                uint32_t va[4];
+                load_tiles_turned(va, vrow + (2 * d / 8) * kPanelOfSlice + ((2 * d % 8 << 4) ^ vunit));
 #pragma unroll
-                for (int d = 0; d < kDt; ++d) {
-                    uint32_t va[4];
-                    load_tiles_turned(va, vals[m] + vrow + (2 * d / 8) * kPanelOfSlice + ((2 * d % 8 << 4) ^ vunit));
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        mma<false>(o[j][d], va, p[m][j][0][0], p[m][j][0][1]);
-                        mma<false>(o[j][d], va, p[m][j][kF8 ? 0 : 1][0], p[m][j][kF8 ? 0 : 1][1]);
-                    }
+                for (int j = 0; j < NT; ++j) {
+                    mma<false>(o[j][d], va, p[j][0][0], p[j][0][1]);
+                    mma<false>(o[j][d], va, p[j][kF8 ? 0 : 1][0], p[j][kF8 ? 0 : 1][1]);
                 }
+            }
         } else {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int d = 0; d < kDt; d += 2) {  // 32 components: the even ones, then the odd ones
+                uint32_t vc[4], va[2][4];
+                load_tiles_turned(vc, vrow + (d / 8) * kPanelOfSlice + ((d % 8 << 4) ^ vunit));
 #pragma unroll
-                for (int d = 0; d < kDt; d += 2) {  // 32 components: the even ones, then the odd ones
-                    uint32_t vc[4], va[2][4];
-                    load_tiles_turned(vc, vals[m] + vrow + (d / 8) * kPanelOfSlice + ((d % 8 << 4) ^ vunit));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {  // bytes (pos 0, d), (pos 0, d + 1), (pos 1, d), (pos 1, d + 1)
-                        const uint32_t x = __byte_perm(vc[e], 0, 0x3120);
-                        va[0][e] = codes_to_f16(x);
-                        va[1][e] = codes_to_f16(x >> 16);
-                    }
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        mma<true>(o[j][d], va[0], p[m][j][0][0], p[m][j][0][1]);
-                        mma<true>(o[j][d + 1], va[1], p[m][j][0][0], p[m][j][0][1]);
-                    }
+                for (int e = 0; e < 4; ++e) {  // bytes (pos 0, d), (pos 0, d + 1), (pos 1, d), (pos 1, d + 1)
+                    const uint32_t x = __byte_perm(vc[e], 0, 0x3120);
+                    va[0][e] = codes_to_f16(x);
+                    va[1][e] = codes_to_f16(x >> 16);
                 }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    mma<true>(o[j][d], va[0], p[j][0][0], p[j][0][1]);
+                    mma<true>(o[j][d + 1], va[1], p[j][0][0], p[j][0][1]);
+                }
+            }
         }
     }
     // component of the output that o[j][d][2 * e + i] of a lane belongs to (query 2t + i): see the tiles above
@@ -1219,7 +1199,6 @@ template <class S, bool TILED, int NT>
 __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S>& sh, int index) {
     using Ti = Tiles<S, NT>;
     constexpr bool kF8 = S::DT == PSMC_F8;
-    constexpr int kMost = NT == 1 || S::DP <= 128 ? S::kPair : 1;  // slices at a time
     const ItemHead it = sh.queue[index % kQueue].head_part;
     const uint8_t* rows = sh.queue[index % kQueue].rows;
     const int lane = pp.lane, warp = pp.warp, t = lane & 3, gq = lane >> 2;
@@ -1252,32 +1231,19 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S
         if (busy) {
             char* at = pp.ring + used * S::kStage;
 #pragma unroll 1
-            for (int m0 = dv.slice; m0 < S::kSlices; m0 += kMost * dv.slices) {
-                uint32_t keys[kMost], vals[kMost], valid[kMost];
-                float k_scale[kMost];
-                int v_byte[kMost];
-                uint32_t any = 0;
-#pragma unroll
-                for (int i = 0; i < kMost; ++i) {
-                    const int m = m0 + i * dv.slices;
-                    keys[i] = smem_of(at) + m * S::kSlice;
-                    vals[i] = keys[i] + S::kHalf;
-                    valid[i] = sh.valid[used][m];
-                    any |= valid[i];
-                    k_scale[i] = 1.f;
-                    v_byte[i] = 127;
-                    if (kF8) {  // lane p's scale bytes
-                        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(at) + 2 * S::kHalf + m * 16 + (lane & 15);
-                        k_scale[i] = __uint_as_float((uint32_t)bytes[0] << 23);
-                        v_byte[i] = bytes[S::kScales];
-                    }
+            for (int m = dv.slice; m < S::kSlices; m += dv.slices) {
+                const uint32_t valid = sh.valid[used][m];
+                if (valid == 0) continue;  // beyond the segment
+                char* keys = at + m * S::kSlice;
+                float k_scale = 1.f;
+                int v_byte = 127;
+                if (kF8) {  // lane p's scale bytes
+                    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(at) + 2 * S::kHalf + m * 16 + (lane & 15);
+                    k_scale = __uint_as_float((uint32_t)bytes[0] << 23);
+                    v_byte = bytes[S::kScales];
                 }
-                if (any == 0) continue;  // beyond the segment
-                if (TILED)
-#pragma unroll
-                    for (int i = 0; i < kMost; ++i)
-                        if (valid[i] != 0xffffu) clear_rows<S>(at + S::kHalf + (m0 + i * dv.slices) * S::kSlice, valid[i], lane);
-                ti.template step<kMost>(q, keys, vals, valid, k_scale, v_byte, lane);
+                if (TILED && valid != 0xffffu) clear_rows<S>(keys + S::kHalf, valid, lane);
+                ti.step(q, smem_of(keys), smem_of(keys) + S::kHalf, valid, k_scale, v_byte, lane);
             }
         }
         next_stage<S>(pp);
@@ -1375,7 +1341,6 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_kernel(const 
 template <class S, bool TILED, int NQ>
 __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, float* qs, float* ps, Pipe& pp, Shared<S>& sh, int index) {
     constexpr int kOwn = S::DP / 32;
-    static_assert(S::kPair == 1, "one slice at a time");
     const ItemHead it = sh.queue[index % kQueue].head_part;
     const uint8_t* rows = sh.queue[index % kQueue].rows;
     const int lane = pp.lane, warp = pp.warp, key = lane & 15, half = lane >> 4, qh4 = NQ == 8 ? half * 4 : 0;
