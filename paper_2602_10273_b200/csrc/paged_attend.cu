@@ -600,6 +600,7 @@ struct Shared {          // beside the ring
     int entries[2][4][S::kSlices];       // table entries of the steps asked for, of either copying warp
     Item queue[kQueue];
     float2 stats[2][kWarps][16];         // {reference, sum} of each warp's queries, of this item and the one before
+    int late;                            // a wait of the arithmetic ran out
 };
 
 // row and query head of query `in_tile` of an item
@@ -832,7 +833,7 @@ struct Pipe {            // the ring of stages as a warp of the arithmetic sees 
     char* ring;
     int stage;           // the stage of the next step
     uint32_t phase;      // its barrier's
-    int worker, warp, lane;
+    int warp, lane;
 };
 template <class S>
 __device__ __forceinline__ bool landed(const Pipe& pp, Shared<S>& sh) { return mbar_wait(&sh.full[pp.stage], pp.phase); }
@@ -1194,9 +1195,9 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& 
     }
 }
 
-// One item, from its queries to its result.  NT: tiles of 8 queries per warp.  false: a wait ran out.
+// One item, from its queries to its result.  NT: tiles of 8 queries per warp.
 template <class S, bool TILED, int NT>
-__device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S>& sh, int index) {
+__device__ __forceinline__ void run_item(const AttendArgs& g, Pipe& pp, Shared<S>& sh, int index) {
     using Ti = Tiles<S, NT>;
     constexpr bool kF8 = S::DT == PSMC_F8;
     const ItemHead it = sh.queue[index % kQueue].head_part;
@@ -1204,7 +1205,6 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S
     const int lane = pp.lane, warp = pp.warp, t = lane & 3, gq = lane >> 2;
     const Division dv(it.nq, S::kGroup, S::kSlices, warp);
     const bool busy = dv.slice < dv.slices && dv.group * S::kGroup < it.nq;
-    bool fine = true;
     RawQueries<S, NT> q;
     if (S::kSlots > 0 && g.q_units) {  // in the slot of the first step's stage, or in a stage before it
         const bool slot = it.nq <= S::kSlotQueries;
@@ -1224,7 +1224,7 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S
     for (int s = 0; s < it.steps; ++s) {
         if (s > 0) release<S>(sh, used, lane);
         if (!landed<S>(pp, sh)) {
-            fine = false;
+            sh.late = 1;
             break;
         }
         used = pp.stage;
@@ -1278,7 +1278,6 @@ __device__ __forceinline__ bool run_item(const AttendArgs& g, Pipe& pp, Shared<S
     }
     if (TILED) fence_async_smem();
     release<S>(sh, used, lane);
-    return fine;
 }
 
 // Sets the CTA up; true for the warps of the arithmetic.
@@ -1289,8 +1288,8 @@ __device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe&
     pp.phase = 0;
     pp.lane = threadIdx.x & 31;
     pp.warp = threadIdx.x >> 5;
-    pp.worker = blockIdx.x;
     if (threadIdx.x == 0) {
+        sh.late = 0;
         for (int i = 0; i < S::kStages; ++i) {
             mbar_init(&sh.full[i], (Feeder<S, TILED>::lane_arrivals(0) ? 33 : 1) + (Feeder<S, TILED>::lane_arrivals(1) ? 33 : 1));
             mbar_init(&sh.empty[i], kWarps);
@@ -1303,6 +1302,14 @@ __device__ __forceinline__ bool open_pipe(const AttendArgs& g, char* smem, Pipe&
     Feeder<S, TILED> feed;
     feed.run(g, pp.ring, sh);
     return false;
+}
+// Before an item: whether its first stage has landed.  The warps meet at barriers inside an item, so that they go into it
+// together or not at all, also where a wait ran out for some of them only.
+template <class S>
+__device__ __forceinline__ bool all_landed(const Pipe& pp, Shared<S>& sh) {
+    if (!landed<S>(pp, sh)) sh.late = 1;
+    sync_warps();
+    return sh.late == 0;
 }
 // A wait for a copy ran out: says so, and gives the copies that are still on their way their time before the CTA ends.
 template <class S>
@@ -1322,16 +1329,13 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_kernel(const 
     Pipe pp;
     if (!open_pipe<S, TILED>(g, smem, pp, sh)) return;
     for (int index = 0;; ++index) {
-        bool fine = landed<S>(pp, sh);
-        if (fine) {
-            if (sh.valid[pp.stage][0] == kEnd) return;
-            fine = sh.queue[index % kQueue].head_part.nq <= 8 ? run_item<S, TILED, 1>(g, pp, sh, index)
-                                                              : run_item<S, TILED, 2>(g, pp, sh, index);
-        }
-        if (!fine) {
+        if (!all_landed<S>(pp, sh)) {
             give_up<S>(g, pp, sh);
             return;
         }
+        if (sh.valid[pp.stage][0] == kEnd) return;
+        if (sh.queue[index % kQueue].head_part.nq <= 8) run_item<S, TILED, 1>(g, pp, sh, index);
+        else run_item<S, TILED, 2>(g, pp, sh, index);
     }
 }
 
@@ -1339,14 +1343,13 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_kernel(const 
 // scores: a lane has one position, and four queries (NQ = 8) or half of the components of four (NQ = 4); in the second
 // product a lane owns DP / 32 components of all queries.
 template <class S, bool TILED, int NQ>
-__device__ __forceinline__ bool run_item_f32(const AttendArgs& g, float* qs, float* ps, Pipe& pp, Shared<S>& sh, int index) {
+__device__ __forceinline__ void run_item_f32(const AttendArgs& g, float* qs, float* ps, Pipe& pp, Shared<S>& sh, int index) {
     constexpr int kOwn = S::DP / 32;
     const ItemHead it = sh.queue[index % kQueue].head_part;
     const uint8_t* rows = sh.queue[index % kQueue].rows;
     const int lane = pp.lane, warp = pp.warp, key = lane & 15, half = lane >> 4, qh4 = NQ == 8 ? half * 4 : 0;
     const Division dv(it.nq, S::kGroup, S::kSlices, warp);
     const int q0 = dv.group * S::kGroup, mine = dv.slice < dv.slices ? min(S::kGroup, it.nq - q0) : 0;  // may be <= 0
-    bool fine = true;
     {
         float x[NQ][kOwn];
 #pragma unroll
@@ -1379,7 +1382,7 @@ __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, float* qs, flo
     for (int st = 0; st < it.steps; ++st) {
         if (st > 0) release<S>(sh, used, lane);
         if (!landed<S>(pp, sh)) {
-            fine = false;
+            sh.late = 1;
             break;
         }
         used = pp.stage;
@@ -1470,7 +1473,6 @@ __device__ __forceinline__ bool run_item_f32(const AttendArgs& g, float* qs, flo
     write_tile<S>(g, it, dv, carry, sh.stats[index & 1], rows, 0, pp);
     if (TILED) fence_async_smem();
     release<S>(sh, used, lane);
-    return fine;
 }
 
 template <class S, bool TILED>
@@ -1483,16 +1485,13 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_f32_kernel(co
     float* qs = reinterpret_cast<float*>(pp.ring + S::kStages * S::kStage) + pp.warp * (8 * S::DP + 16 * 8);  // [8][DP]
     float* ps = qs + 8 * S::DP;                                                                               // [16][8]
     for (int index = 0;; ++index) {
-        bool fine = landed<S>(pp, sh);
-        if (fine) {
-            if (sh.valid[pp.stage][0] == kEnd) return;
-            fine = sh.queue[index % kQueue].head_part.nq <= 4 ? run_item_f32<S, TILED, 4>(g, qs, ps, pp, sh, index)
-                                                              : run_item_f32<S, TILED, 8>(g, qs, ps, pp, sh, index);
-        }
-        if (!fine) {
+        if (!all_landed<S>(pp, sh)) {
             give_up<S>(g, pp, sh);
             return;
         }
+        if (sh.valid[pp.stage][0] == kEnd) return;
+        if (sh.queue[index % kQueue].head_part.nq <= 4) run_item_f32<S, TILED, 4>(g, qs, ps, pp, sh, index);
+        else run_item_f32<S, TILED, 8>(g, qs, ps, pp, sh, index);
     }
 }
 
