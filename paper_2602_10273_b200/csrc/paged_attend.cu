@@ -928,6 +928,19 @@ __device__ __forceinline__ void load_queries(const AttendArgs& g, const ItemHead
     }
 }
 
+// The factor 2^by, by <= 0, that takes sums and outputs from one reference to a larger one.  8-bit caches: references hold the
+// values' scales, so two of them may lie 2^128 apart although the sums that belong to them are of one size; a sum is moved in
+// two steps of half the way each.
+template <int DT>
+struct Moved {
+    float step, rest;
+    __device__ __forceinline__ explicit Moved(float by) {
+        step = exp2f(DT == PSMC_F8 ? 0.5f * by : by);
+        rest = DT == PSMC_F8 ? step : 1.f;
+    }
+    __device__ __forceinline__ float sum(float x) const { return x * step * rest; }
+    __device__ __forceinline__ float factor() const { return step * rest; }
+};
 template <class S, int NT>
 struct Tiles {
     static constexpr bool kF8 = S::DT == PSMC_F8;
@@ -1011,8 +1024,8 @@ struct Tiles {
             const int b0 = __shfl_sync(kFull, v_byte, gq), b1 = __shfl_sync(kFull, v_byte, gq + 8);
             ev0 = (float)(b0 - 127);
             ev1 = (float)(b1 - 127);
-            iv0 = ok0 ? __uint_as_float((uint32_t)(254 - b0) << 23) : 0.f;
-            iv1 = ok1 ? __uint_as_float((uint32_t)(254 - b1) << 23) : 0.f;
+            iv0 = ok0 ? __uint_as_float((uint32_t)(254 - kScaleLimit - b0) << 23) : 0.f;
+            iv1 = ok1 ? __uint_as_float((uint32_t)(254 - kScaleLimit - b1) << 23) : 0.f;
         }
         bool grow = false;
 #pragma unroll
@@ -1036,9 +1049,10 @@ struct Tiles {
                     top = fmaxf(top, __shfl_xor_sync(kFull, top, 16));
                     // each query by itself: another one of the tile, or a column that none uses, does not change its roundings
                     if (!(top > ref[j][i] + kSlack)) top = ref[j][i];
-                    const float f = top == ref[j][i] ? 1.f : ex2(ref[j][i] - top);
+                    const Moved<S::DT> to(top == ref[j][i] ? 0.f : ref[j][i] - top);
+                    const float f = to.factor();
                     ref[j][i] = top;
-                    sum[j][i] *= f;
+                    sum[j][i] = to.sum(sum[j][i]);
 #pragma unroll
                     for (int d = 0; d < kDt; ++d) {
                         o[j][d][i] *= f;
@@ -1050,16 +1064,18 @@ struct Tiles {
         uint32_t p[NT][kF8 ? 1 : 2][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const float r0 = ref[j][0] == -INFINITY ? 0.f : ref[j][0], r1 = ref[j][1] == -INFINITY ? 0.f : ref[j][1];
+            constexpr float kUp = kF8 ? kScaleLimit : 0.f;
+            const float r0 = ref[j][0] == -INFINITY ? 0.f : ref[j][0] - kUp, r1 = ref[j][1] == -INFINITY ? 0.f : ref[j][1] - kUp;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float p0 = ex2(s[j][2 * h] - r0), p1 = ex2(s[j][2 * h + 1] - r1);
                 if (kF8) {
                     // weights of the codes: the values' scale is in the exponent already, and the sum takes it out again; fp16
-                    // holds 11 bits of a weight down to 2^-14 of the largest
+                    // holds 11 bits of a weight down to 2^-14 of the largest.  They are formed 2^60 times too large, so that
+                    // one that counts in the sum, but whose values are 2^-120 of another's, is no subnormal number.
                     sum[j][0] = fmaf(p0, h ? iv1 : iv0, sum[j][0]);
                     sum[j][1] = fmaf(p1, h ? iv1 : iv0, sum[j][1]);
-                    p[j][0][h] = turn_tile(pack_f16(p0, p1));
+                    p[j][0][h] = turn_tile(pack_f16(p0 * pow2i(-kScaleLimit), p1 * pow2i(-kScaleLimit)));
                 } else {
                     // a weight as the sum of two bf16 numbers: 16 bits of it instead of 8
                     sum[j][0] += p0;
@@ -1154,8 +1170,9 @@ __device__ __forceinline__ void write_tile(const AttendArgs& g, const ItemHead& 
             for (int z = 0; z < kWarps; ++z)
                 if (z < dv.slices) {
                     // (a factor of zero keeps a NaN that came with the values)
-                    const float f = st[z].x == top[v] ? 1.f : (st[z].x == -INFINITY ? 0.f : ex2(st[z].x - top[v]));
-                    total[v] = fmaf(st[z].y, f, total[v]);
+                    const Moved<S::DT> to(st[z].x == top[v] ? 0.f : st[z].x - top[v]);
+                    const float f = to.factor();
+                    total[v] += to.sum(st[z].y);
 #pragma unroll
                     for (int i = 0; i < kOwn; ++i) {
                         const int d = pp.lane * 4 + i * 128;
@@ -1575,9 +1592,10 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
             }
             if (slot >= 0) st = g.l.stat[slot];
             // into the running result: the largest reference decides, the others' weights are 2^(their reference - it)
-            const float high = fmaxf(top, warp_max(st.x)), keep = top == high ? 1.f : exp2f(top - high);
-            const float f = st.x == -INFINITY ? 0.f : (st.x == high ? 1.f : exp2f(st.x - high));
-            total = fmaf(total, keep, warp_sum(st.y * f));
+            const float high = fmaxf(top, warp_max(st.x));
+            const Moved<DT> held(top == high ? 0.f : top - high), to(st.x == high ? 0.f : st.x - high);
+            const float keep = held.factor(), f = to.factor();
+            total = held.sum(total) + warp_sum(to.sum(st.y));
             top = high;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) o[i] = float4{o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep};
@@ -1623,8 +1641,9 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
         for (int i = 0; i < kOwn; ++i) o[i] = float4{0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < WPQ; ++w) {
             const float2 st = stats[w];
-            const float f = st.x == -INFINITY ? 0.f : (st.x == top ? 1.f : exp2f(st.x - top));
-            total = fmaf(st.y, f, total);
+            const Moved<DT> to(st.x == top ? 0.f : st.x - top);
+            const float f = to.factor();
+            total += to.sum(st.y);
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
                 const float4 x = *reinterpret_cast<const float4*>(&acc[w][lane * 4 + i * 128]);
@@ -1704,7 +1723,7 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.l.ls = LineShape{S::kStep, S::kGroup, a.Hq / c.H, c.H};
     g.by_ratio = fast_div(g.l.ls.ratio);
     g.by_heads = fast_div(a.Hq);
-g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
+    g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
     g.q_units = ((uint64_t)(uintptr_t)a.q.data % 16 == 0 && a.q.stride_row % 8 == 0 && a.q.stride_head % 8 == 0 && c.D % 8 == 0) ? 1 : 0;
     TilePlan* plans = reinterpret_cast<TilePlan*>(scratch + sc.plans);
     g.l.plans = plans;

@@ -18,6 +18,17 @@ IO = {"f32": torch.float32, "bf16": torch.bfloat16, "f8": torch.bfloat16}
 WEIGHT_STEP = {"f32": 0.0, "bf16": 2.0 ** -16, "f8": 2.0 ** -11 + 4096 * 2.0 ** -25}
 
 
+def f8_blocks(x):
+    """[blocks, H, page, D] -> the same as 8-bit blocks."""
+    n, H, page, D = x.shape
+    e, q = PR.quantise(x.double())
+    y = torch.ldexp(q, -e[..., None])          # codes as values
+    raw = torch.zeros((n, B.paged_block_bytes(H, page, D, B.F8)), dtype=torch.uint8, device="cuda")
+    raw[:, : H * page * D] = y.float().to(torch.float8_e4m3fn).view(torch.uint8).view(n, -1)
+    raw[:, H * page * D: H * page * D + H * page] = (e + 127).to(torch.uint8).view(n, -1)
+    return raw
+
+
 class Cache:
     """Random pools, table and lengths.  share: rows r with equal r // share use the same blocks where both are full."""
 
@@ -46,12 +57,7 @@ class Cache:
             x = torch.randn(shape, device="cuda", generator=g) * magnitude
             if dt == "f8":
                 x = x * torch.exp2(torch.randint(-6, 7, shape[:3] + (1,), device="cuda", generator=g).float())
-                e, q = PR.quantise(x.double())
-                y = torch.ldexp(q, -e[..., None])          # codes as values
-                raw = torch.zeros((self.n_blocks, B.paged_block_bytes(H, page, D, B.F8)), dtype=torch.uint8, device="cuda")
-                raw[:, : H * page * D] = y.float().to(torch.float8_e4m3fn).view(torch.uint8).view(self.n_blocks, -1)
-                raw[:, H * page * D: H * page * D + H * page] = (e + 127).to(torch.uint8).view(self.n_blocks, -1)
-                x = raw
+                x = f8_blocks(x)
             else:
                 x = x.to(IO[dt])
             self.pools.append(x)
@@ -176,6 +182,30 @@ def test_attend_large_scores_and_far_maxima(dt):
     q = (12 * torch.randn((4, ratio, D), device="cuda")).to(IO[dt])
     out = B.paged_attend(c.handle, q, c.lens, 1.0)
     check_attend(c, q, out, None, 1.0)
+
+
+@pytest.mark.parametrize("len_, room", [(3000, 0), (900, 0), (900, 200)])
+def test_attend_8bit_values_of_any_size(len_, room):
+    """One position's values are 2^122 of the others', which carry most of the softmax's sum: at the row's start,
+    middle and end, and in no position of the last row."""
+    R, H, D, page = 4, 2, 64, 16
+    c = Cache("f8", [len_] * R, H, D, page, seed=2, spare_cols=room)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k = 0.02 * torch.randn((c.n_blocks, H, page, D), device="cuda", generator=g)
+    v = torch.randn(k.shape, device="cuda", generator=g) * 2.0 ** -56
+    k[..., 0] = 0
+    for r, p in enumerate([0, len_ // 2, len_ - 1]):
+        block, at = int(c.table[r, p // page]), p % page
+        k[block, :, at, 0] = 1.0
+        v[block, :, at] *= 2.0 ** 122
+    c.pools[0].copy_(f8_blocks(k))
+    c.pools[1].copy_(f8_blocks(v))
+    q = torch.randn((R, 3 * H, D), device="cuda", generator=g)
+    q[..., 0] = 0.875 * math.log(len_) * D ** 0.5
+    q = q.bfloat16()
+    lse = torch.empty((R, 3 * H), device="cuda")
+    out = B.paged_attend(c.handle, q, c.lens, D ** -0.5, lse=lse)
+    check_attend(c, q, out, lse, D ** -0.5)
 
 
 def test_attend_does_not_mix_rows_or_heads_that_hold_nan():
