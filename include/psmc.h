@@ -294,7 +294,8 @@ const int32_t* psmc_kv_paged_free_count(psmc_ctx*); /* [1] blocks on the free li
  * power of two that brings the head's largest finite component to at most 448, with the exponent kept within [-60, 60]
  * (larger components saturate, smaller ones round to zero); components that are not finite become NaN.
  *
- * head_dim at most 256, and head_dim times the element size of the pool a multiple of 16 bytes; pools 16-byte aligned.
+ * head_dim at most 256, and head_dim times the element size of the pool a multiple of 16 bytes; pools 16-byte aligned;
+ * a block's elements at most 1 GiB, max_blocks * block_len below 2^31.
  * A table entry that a call needs and that names no block (negative, or n_blocks and beyond), and a length beyond the
  * table, raise PSMC_E_STATE in the status word: such positions are neither written nor read, the rest is done. */
 typedef struct {
@@ -345,8 +346,8 @@ psmc_status psmc_rope_frequencies(psmc_rope_scaling kind, int rot_dim, double th
  * get their rotary positions (rope NULL: none) and go into the cache with its values v; its queries q [n, Hq, D], when
  * given, get theirs into q_out, which may be q itself.  Angles are formed in 64 bits.  Tokens with rows[i] < 0 are padding, and
  * tokens of rows with skip[row] != 0 (DEVICE [R], may be NULL) are left out: nothing of theirs is written.
- * The block of a position must belong to the row alone or be written by one of its owners only; a position that appears
- * twice in a call gets one of the two tokens. */
+ * The block of a position must belong to the row alone or be written by one of its owners only, and the tokens of a call
+ * must be different positions: of one that appears twice the cache holds parts of either afterwards. */
 psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows, const int32_t* positions,
                              const uint8_t* skip, const psmc_rope* rope, const psmc_heads* k, const psmc_heads* v,
                              int n_q_heads, const psmc_heads* q, const psmc_heads* q_out, int32_t* status_word, void* stream);
@@ -354,8 +355,8 @@ psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows
 /* out[r, h] = sum_p softmax_p(scale * q[r, h] . k_p) v_p over the positions p < lens[r] + extra of row r, for query heads
  * h = 0 .. Hq-1 (a multiple of H: head h reads key-value head h / (Hq / H)).  lse (DEVICE [R, Hq] fp32, may be NULL)
  * receives ln sum_p exp(scale * q . k_p), so that results over parts of a context can be joined.  A row without
- * positions gets zeros and lse = -inf; rows with skip[r] != 0 are left as they were.  Blocks that several rows share are
- * read once for all of them where they lie within a run of 32 rows.  scratch: psmc_paged_attend_scratch_bytes() bytes,
+ * positions gets zeros and lse = -inf; rows with skip[r] != 0 are left as they were.  Leading blocks that rows of one run of 32 (rows 32 i .. 32 i + 31)
+ * share are read once for all of them, unless so few rows of so little room are asked for that it would not pay.  scratch: psmc_paged_attend_scratch_bytes() bytes,
  * 256-byte aligned, contents irrelevant; calls that may overlap (other streams, graphs replayed side by side) need
  * scratch of their own.  out may not overlap q.  max_blocks * block_len and R * Hq up to 2^27. */
 size_t psmc_paged_attend_scratch_bytes(int R, int n_q_heads, int n_kv_heads, int head_dim);

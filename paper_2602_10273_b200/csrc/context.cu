@@ -628,9 +628,9 @@ psmc_status view_of(const psmc_paged_kv* kv, PagedView* out) {
     const int elem = pool_elem_bytes(kv->dt);
     if (((uint64_t)(uintptr_t)kv->k | (uint64_t)(uintptr_t)kv->v | (uint64_t)(kv->head_dim * elem)) % 16 != 0) return PSMC_E_INVAL;
     if ((uint64_t)(uintptr_t)kv->table % 4 != 0) return PSMC_E_INVAL;
-    // positions, and the elements of one block, are counted in an int
+    // positions, and the elements of one block with a CTA's stride to spare, are counted in an int
     if ((int64_t)kv->max_blocks * kv->block_len >= ((int64_t)1 << 31) ||
-        (int64_t)kv->n_kv_heads * kv->block_len >= ((int64_t)1 << 31) / kv->head_dim / elem)
+        (int64_t)kv->n_kv_heads * kv->block_len > ((int64_t)1 << 30) / kv->head_dim / elem)
         return PSMC_E_INVAL;
     PagedView& c = *out;
     c.k = static_cast<char*>(kv->k); c.v = static_cast<char*>(kv->v);
