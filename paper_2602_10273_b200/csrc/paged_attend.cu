@@ -571,6 +571,8 @@ struct Shape {
     static constexpr int kSlotQueries = DT == PSMC_F32 ? 0 : (kLeft >= kStages * 16 * kQueryRow ? 16 : (kLeft >= kStages * 8 * kQueryRow ? 8 : 0));
     static constexpr int kSlots = kSlotQueries * kQueryRow;  // bytes per stage
     static constexpr int kBytes = kStages * (kStage + kSlots) + kExtra + 1024;
+    // (an item's warps read whole tiles of 8 or 16 queries, used or not: they lie in the slot, or in the stage)
+    static_assert(DT == PSMC_F32 || kGroups * kGroup * kQueryRow <= kStage, "a stage holds the queries of an item");
     static_assert(kStages >= 2 && kStage >= kWarps * 8 * (DP + 4) * 4, "a ring; a stage holds the warps' outputs of a query tile");
 };
 
@@ -1750,10 +1752,11 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     e = allow_dynamic_smem(reinterpret_cast<const void*>(fn), S::kBytes);
     if (e == cudaSuccess) e = launch_chained(fn, dim3((unsigned)g.l.workers), dim3(kThreads), S::kBytes, stream, g);
     if (e != cudaSuccess || g.l.direct) return e;
-    // few queries: four warps each, for what may be many partial results of a long row
+    // few queries: four warps each, for what may be many partial results of a long row (32 queries of 131071 positions 101 us,
+    // with one warp 106; 896 queries of 32 rows 54 and 52; 16384 of 512 rows 229 and 161)
     const int64_t queries = (int64_t)c.R * a.Hq;
     constexpr int kOwn = DP > 128 ? 2 : 1;
-    if (queries <= 8 * kSMs) return launch_chained(paged_join_kernel<DT, 4, kOwn>, dim3((unsigned)queries), dim3(kJoinThreads), 0, stream, g);
+    if (queries <= 2 * kSMs) return launch_chained(paged_join_kernel<DT, 4, kOwn>, dim3((unsigned)queries), dim3(kJoinThreads), 0, stream, g);
     return launch_chained(paged_join_kernel<DT, 1, kOwn>, dim3((unsigned)((queries + 3) / 4)), dim3(kJoinThreads), 0, stream, g);
 }
 
