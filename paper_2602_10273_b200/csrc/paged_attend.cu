@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
     };
     __shared__ Found found[kPlanWarps][kWarpSegs];
     __shared__ Found segs[kMaxSegs];
-    __shared__ int count[kPlanWarps], rows_in[kPlanWarps], ends[kMaxSegs], n_of[kTileRows];
+    __shared__ int count[kPlanWarps], rows_in[kPlanWarps], ends[kMaxSegs], n_of[kTileRows], n_alive;
     chain_begin();
     const int tile = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = c.block_len;
     TilePlan& tp = plans[tile];
@@ -110,6 +110,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
             e[u] = is_row && j >= 0 && j < c.max_blocks ? __ldg(entries + j) : -1;
         }
     };
+    const int entry0 = is_row ? __ldg(entries) : -1;
     fetch(warp * kRun);
     int64_t len = is_row ? (int64_t)__ldg(a.lens + row) + a.extra : 0;
     const bool left_out = !is_row || (a.skip && a.skip[row]);
@@ -120,8 +121,13 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
         len = room;
     }
     const int n = (int)len;
-    if (warp == 0) n_of[lane] = n;
+    // (Every warp reads the lengths.  What is written by them goes by the first warp's, so that lengths which somebody changes
+    // meanwhile, against the rules, give wrong results but no wrong addresses.)
     const uint32_t alive = __ballot_sync(kFull, n > 0), out_mask = __ballot_sync(kFull, left_out);
+    if (warp == 0) {
+        n_of[lane] = n;
+        n_alive = __popc(alive);
+    }
     const int nb = warp_max((n + B - 1) / B);
 
     // How this row stands in block j: positions of it that count, and the block's number, if it has one that exists.
@@ -134,12 +140,14 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
         return live > 0 ? same & alike : 0u;
     };
     int begun = 0, rows = 0;
-    if (__popc(alive) > 1) {
+    // Rows that part in block 0 stay apart: where all do, none of them shares anything, and the table need not be looked at
+    // any further (64 rows of 4096 positions 13 -> 6 us).
+    const uint32_t set0 = all_like(name_of(entry0, live_in(0)), live_in(0));
+    if (__any_sync(kFull, (set0 & (set0 - 1)) != 0)) {
         for (int j0 = warp * kRun; j0 < nb; j0 += kPlanWarps * kRun) {
             if (j0 >= kPlanWarps * kRun) fetch(j0);
             uint32_t set = 0;
             if (j0 > 0) set = all_like(name_of(e[0], live_in(j0 - 1)), live_in(j0 - 1));
-            else set = alive;  // before the first block all rows are one set; block 0 begins a segment in any case
 #pragma unroll
             for (int u = 0; u < kRun; ++u) {
                 const int j = j0 + u, live = live_in(j), name = name_of(e[u + 1], live);
@@ -147,26 +155,28 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
                 // Sets only ever split: copy-on-write keeps two rows apart once they have parted, and in any other table
                 // two sets that meet again are just read apart.  A set splits where some row of it does not stand like its
                 // first row; its pieces are taken off one by one, first rows first.
-                const uint32_t prev = j == 0 ? 0u : set;
-                {
+                const uint32_t prev = set;
+                if (j == 0) {
+                    set = set0;  // every set begins here
+                } else {
                     const int lead = set ? __ffs(set) - 1 : lane;
                     const int lead_name = __shfl_sync(kFull, name, lead), lead_live = __shfl_sync(kFull, live, lead);
-                    if (j > 0 && __all_sync(kFull, set == 0 || (name == lead_name && live == lead_live))) continue;  // as before
-                }
-                uint32_t open = __ballot_sync(kFull, set != 0), mine = set;
-                if (live == 0) set = 0;
-                for (int piece = 0; open && piece < kTileRows; ++piece) {
-                    const int lead = mine ? __ffs(mine) - 1 : lane;
-                    const int lead_name = __shfl_sync(kFull, name, lead), lead_live = __shfl_sync(kFull, live, lead);
-                    const bool like = name == lead_name && live == lead_live;
-                    const uint32_t alike = __ballot_sync(kFull, mine != 0 && like);
-                    if (mine != 0 && like) {
-                        if (live > 0) set = mine & alike;
-                        mine = 0;
-                    } else {
-                        mine &= ~alike;
+                    if (__all_sync(kFull, set == 0 || (name == lead_name && live == lead_live))) continue;  // as before
+                    uint32_t open = __ballot_sync(kFull, set != 0), mine = set;
+                    if (live == 0) set = 0;
+                    for (int piece = 0; open && piece < kTileRows; ++piece) {
+                        const int lead = mine ? __ffs(mine) - 1 : lane;
+                        const int lead_name = __shfl_sync(kFull, name, lead), lead_live = __shfl_sync(kFull, live, lead);
+                        const bool like = name == lead_name && live == lead_live;
+                        const uint32_t alike = __ballot_sync(kFull, mine != 0 && like);
+                        if (mine != 0 && like) {
+                            if (live > 0) set = mine & alike;
+                            mine = 0;
+                        } else {
+                            mine &= ~alike;
+                        }
+                        open = __ballot_sync(kFull, mine != 0);
                     }
-                    open = __ballot_sync(kFull, mine != 0);
                 }
                 const bool begins = set != 0 && set != prev && lane == __ffs(set) - 1;
                 const uint32_t who = __ballot_sync(kFull, begins);
@@ -192,7 +202,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
     const float all_rows = warp_sum(lane < kPlanWarps ? (float)rows_in[lane] : 0.f);
     const bool by_row = n_segs == 0 || n_segs > kMaxSegs || all_rows > kTileRows * kRowSegs || warp_max(mine) > kWarpSegs;
     if (by_row) {
-        n_segs = __popc(alive);
+        n_segs = n_alive;
         if (warp == 0 && n > 0) segs[__popc(alive & ((1u << lane) - 1))] = Found{1u << lane, 0, lane};
     } else {
         const int at = __shfl_sync(kFull, upto - mine, warp);
@@ -206,7 +216,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedVie
         for (int o = lane; o < n_segs; o += 32)
             if (segs[o].from > f.from && (segs[o].mask >> f.lead & 1)) end = min(end, segs[o].from);
         end = __reduce_min_sync(kFull, end);
-        if (lane == 0) ends[s] = min(end * B, len);
+        if (lane == 0) ends[s] = max(f.from * B, min(end * B, len));
     }
     __syncthreads();
     if (warp == 0) {
