@@ -15,7 +15,7 @@
 //           warp, and where that leaves warps over, by positions.
 //   join    per (row, query head): the partial results of the row's segments and of the shares that split them.
 //
-// Few rows of short capacity take the middle kernel alone, a CTA for each (row, key-value head): see launch().
+// Few rows take the middle kernel alone, a CTA for each (row, key-value head): see launch().
 //
 // Scores and outputs are formed transposed, S^T = K Q^T and O^T = V^T P^T, on the warp-level matrix instructions: the 16
 // rows of an operand tile are positions (or components of the output) and its 8 columns queries, so that the 4 to 8
@@ -1744,12 +1744,16 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.l.first_rest = sc.first_rest;
     g.l.n_tiles = sc.n_tiles;
     g.l.workers = S::kCtas * kSMs;
-    // A grid of one CTA per (row, key-value head, query tile) that fits the GPU at once, over rows of at most 16 steps: what
-    // splitting and sharing would save is less than the two other kernels cost (4 fp32 rows of 121 positions 17 -> 8 us, 8 rows
-    // of 1000 positions with 32 heads each 23 -> 17 us; the results do not depend on the lengths at hand, which only the device
-    // knows, but on the room that the table has).
+    // One CTA per (row, key-value head, query tile), all resident at once, and nothing else: no plan, no join, no cutting.  What
+    // that leaves idle (the CTAs that there is no such item for, over the steps that the table has room for) may be worth 20
+    // steps of the whole GPU, which is what the rest costs: 4 fp32 rows of 121 positions 17 -> 6 us, 8 bf16 rows of 1000
+    // positions with 32 heads each 24 -> 16, 16 of 2048 with 8 heads 44 -> 29, 36 of 4096 with 8 heads 115 -> 92; and beyond it
+    // 4 of 2048 22 -> 26, 8 8-bit rows of 4096 with 4 heads 25 -> 39.  Blocks that rows share come from L2 then (32 rows of 2048
+    // positions, 9 of 10 blocks shared: 45 -> 29 us).  64 steps at most: which rows are short only the device knows, and a
+    // single long one would take a CTA that time.
     const int64_t direct = (int64_t)c.R * c.H * ((g.l.ls.ratio + kGroups * S::kGroup - 1) / (kGroups * S::kGroup));
-    g.l.direct = direct <= g.l.workers && (int64_t)c.max_blocks * c.block_len <= 16 * S::kStep ? 1 : 0;
+    const int64_t room = (int64_t)c.max_blocks * c.block_len, idle = g.l.workers - direct;
+    g.l.direct = idle >= 0 && room <= 64 * S::kStep && room * idle <= (int64_t)20 * S::kStep * g.l.workers ? 1 : 0;
     if (g.l.direct) g.l.workers = (int)direct;
     cudaError_t e = g.l.direct ? cudaSuccess : launch_chained(paged_plan_kernel<DT>, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
     if (e != cudaSuccess) return e;

@@ -1,6 +1,9 @@
 """Rotary write, attention and read-back on the paged cache, against the 64-bit definitions of tests/paged_reference.py."""
 import ctypes as C
 import math
+import pathlib
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -29,6 +32,7 @@ def f8_blocks(x):
     return raw
 
 
+# Tables of many spare columns make attention take its split form, whatever the lengths.
 class Cache:
     """Random pools, table and lengths.  share: rows r with equal r // share use the same blocks where both are full."""
 
@@ -136,7 +140,7 @@ SHAPES = [  # dt, H, queries per key-value head, D, page, lens, share
 @pytest.mark.parametrize("dt,H,ratio,D,page,lens,share", SHAPES, ids=lambda v: str(v)[:24].replace(" ", ""))
 def test_attend(dt, H, ratio, D, page, lens, share, room):
     """room: a table hardly wider than the rows need, or one wide enough for the split form whatever the lengths."""
-    c = Cache(dt, lens, H, D, page, seed=5, share=share, spare_cols=3 if room == "tight" else 3 + 2048 // page)
+    c = Cache(dt, lens, H, D, page, seed=5, share=share, spare_cols=3 if room == "tight" else 3 + 8192 // page)
     g = torch.Generator(device="cuda").manual_seed(9)
     q = (1.5 * torch.randn((c.R, H * ratio, D), device="cuda", generator=g)).to(IO[dt])
     lse = torch.full((c.R, H * ratio), 7.0, device="cuda")
@@ -149,11 +153,12 @@ def test_attend(dt, H, ratio, D, page, lens, share, room):
     assert torch.equal(out, again)                      # the same bits every time: no sum depends on an order of arrival
 
 
+@pytest.mark.parametrize("spare", [0, 512])
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f8"])
-def test_attend_strides_skip_extra_and_scale(dt):
+def test_attend_strides_skip_extra_and_scale(dt, spare):
     """Queries that are part of a projection's output, an out with gaps, finished rows, the position just written."""
     H, ratio, D, page = 2, 4, 64, 16
-    c = Cache(dt, [40, 17, 300, 16, 16], H, D, page, seed=3)
+    c = Cache(dt, [40, 17, 300, 16, 16], H, D, page, seed=3, spare_cols=spare)
     c.lens -= 1                                         # extra = 1 restores it
     qkv = torch.randn((5, (ratio + 2) * H, D), device="cuda").to(IO[dt])
     q = qkv[:, : ratio * H]
@@ -174,17 +179,18 @@ def test_attend_strides_skip_extra_and_scale(dt):
     assert torch.equal(B.paged_attend(c.handle, odd, c.lens, 0.3, extra=1), B.paged_attend(c.handle, q.contiguous(), c.lens, 0.3, extra=1))
 
 
+@pytest.mark.parametrize("spare", [0, 512])
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f8"])
-def test_attend_large_scores_and_far_maxima(dt):
+def test_attend_large_scores_and_far_maxima(dt, spare):
     """Scores of hundreds, the maximum at the first, a middle and the last position, other rows' scores very negative."""
     H, ratio, D, page = 1, 4, 64, 16
-    c = Cache(dt, [200, 200, 200, 200], H, D, page, seed=11, magnitude=4.0)
+    c = Cache(dt, [200, 200, 200, 200], H, D, page, seed=11, magnitude=4.0, spare_cols=spare)
     q = (12 * torch.randn((4, ratio, D), device="cuda")).to(IO[dt])
     out = B.paged_attend(c.handle, q, c.lens, 1.0)
     check_attend(c, q, out, None, 1.0)
 
 
-@pytest.mark.parametrize("len_, room", [(3000, 0), (900, 0), (900, 200)])
+@pytest.mark.parametrize("len_, room", [(3000, 0), (900, 0), (900, 512)])
 def test_attend_8bit_values_of_any_size(len_, room):
     """One position's values are 2^122 of the others', which carry most of the softmax's sum: at the row's start,
     middle and end, and in no position of the last row."""
@@ -208,11 +214,12 @@ def test_attend_8bit_values_of_any_size(len_, room):
     check_attend(c, q, out, lse, D ** -0.5)
 
 
-def test_attend_does_not_mix_rows_or_heads_that_hold_nan():
+@pytest.mark.parametrize("spare", [0, 512])
+def test_attend_does_not_mix_rows_or_heads_that_hold_nan(spare):
     """A NaN in a live key or value reaches the heads that read it, and nothing else."""
     H, ratio, D, page = 2, 4, 64, 16
     for dt in ("f32", "bf16", "f8"):
-        c = Cache(dt, [100, 100, 100, 100], H, D, page, seed=2, share=4)
+        c = Cache(dt, [100, 100, 100, 100], H, D, page, seed=2, share=4, spare_cols=spare)
         q = torch.randn((4, H * ratio, D), device="cuda").to(IO[dt])
         clean = B.paged_attend(c.handle, q, c.lens, 0.1)
         blk = int(c.table[2, 6])                        # the last block: row 2's own
@@ -227,10 +234,11 @@ def test_attend_does_not_mix_rows_or_heads_that_hold_nan():
         assert torch.equal(out[keep], clean[keep])
 
 
+@pytest.mark.parametrize("spare", [0, 512])
 @pytest.mark.parametrize("dt", ["bf16", "f8"])
-def test_attend_reports_bad_tables_and_lengths(dt):
+def test_attend_reports_bad_tables_and_lengths(dt, spare):
     H, D, page = 2, 64, 16
-    c = Cache(dt, [64, 64, 64], H, D, page, seed=1)
+    c = Cache(dt, [64, 64, 64], H, D, page, seed=1, spare_cols=spare)
     q = torch.randn((3, 4, D), device="cuda").to(IO[dt])
     good = B.paged_attend(c.handle, q, c.lens, 0.1)
     for bad in (-1, -(1 << 31), c.n_blocks, (1 << 31) - 1):
@@ -660,3 +668,40 @@ def test_the_binding_refuses_what_does_not_fit():
         B.PagedKv(c.pools[0], c.pools[1][:1], c.table, 2, 64, 16)
     with pytest.raises(AssertionError):
         B.paged_read(c.handle, c.lens, torch.zeros((2, 2, 64, 40), dtype=torch.bfloat16, device="cuda").transpose(2, 3))
+
+
+FIRST_IN_A_CAPTURE = """
+import torch
+from paper_2602_10273_b200 import binding as B
+H, Hq, D, page, R = 2, 8, 64, 16, 3
+pools = [torch.zeros((40, H, page, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+wide = torch.arange(30, dtype=torch.int32, device="cuda").view(R, 10).repeat(1, 60)
+lens = torch.tensor([150, 0, 33], dtype=torch.int32, device="cuda")
+x = [torch.randn((R, n, D), device="cuda").bfloat16() for n in (Hq, H, H)]
+k, v = [torch.zeros((R, H, 160, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+outs = [torch.empty((R, Hq, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+kv, kv_wide = [B.PagedKv(pools[0], pools[1], t, H, D, page) for t in (wide[:, :10].contiguous(), wide)]
+turned = torch.empty_like(x[0])
+torch.cuda.synchronize()
+def calls():
+    B.paged_write(kv, x[1], x[2], None, lens, q=x[0], q_out=turned)
+    B.paged_attend(kv, turned, lens, 0.125, out=outs[0], extra=1)
+    B.paged_attend(kv_wide, turned, lens, 0.125, out=outs[1], extra=1)
+    B.paged_read(kv, lens, k_out=k, v_out=v)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    calls()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in outs + pools + [k[0], v[0]]]
+calls()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, outs + pools + [k[0], v[0]]))
+assert outs[0].abs().sum() > 0
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    done = subprocess.run([sys.executable, "-c", FIRST_IN_A_CAPTURE], cwd=pathlib.Path(__file__).parent.parent, timeout=120,
+                          stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert done.returncode == 0, done.stdout[-2000:]
