@@ -19,10 +19,20 @@
 //
 // Scores and outputs are formed transposed, S^T = K Q^T and O^T = V^T P^T, on the warp-level matrix instructions: the 16
 // rows of an operand tile are positions (or components of the output) and its 8 columns queries, so that the 4 to 8
-// queries of one key-value head fill a tile, and K and V come straight from their rows in shared memory.  (These
-// instructions reach a fraction of the tensor cores' rate, and a fraction is enough: at 4 queries per head the arithmetic
-// of a step is 1/10 of the time its bytes take.)  A weight is exp2(s - m) with m a reference per query that follows the
-// largest score only when it is exceeded by more than 8 (a rare, warp-uniform branch); sums and outputs are fp32.
+// queries of one key-value head fill a tile, and K and V come straight from their rows in shared memory, the output of a
+// warp's queries staying in its registers.  A tile of 128 rows, as the units with their own accumulator memory want it,
+// would be all but empty here, or filled with positions at the price of taking every score through that memory and back.
+// What these instructions can do is no bound: m16n8k16 issues 1.9 times per clock and SM (measured; 2.2 Pflop/s), and at 4
+// queries per head the products of a step take a tenth of the time its bytes do.  A weight is exp2(s - m) with m a
+// reference per query that follows the largest score only when it is exceeded by more than 8 (a rare, warp-uniform
+// branch); sums and outputs are fp32.
+//
+// Measured (in a graph; copy rate of this GPU 6.56 TB/s): one row of 131071 positions, 32 query and 8 key-value heads of 128,
+// bf16, 102 us = 5.3 TB/s, of which the middle kernel 91; 36 rows of 4096 in the one-kernel form 92 us = 6.6 TB/s; 512 rows in
+// groups of 8 that share half, 64 to 1280 positions, 153 us (distinct blocks alone 67: items are short there, and putting one
+// together costs as much as 1 to 3 steps); 256 rows of 1 to 2303 positions, 8-bit, 138 us = 4.4 TB/s (conversions of codes
+// issue beside the products); 32 rows of 4211 positions of one ancestry, 28 query heads, 8-bit, 49 us (in the one-kernel form,
+// each row reading its blocks from L2).
 #include <cuda.h>
 
 #include "bulk_copy.cuh"
@@ -1525,21 +1535,24 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_f32_kernel(co
 }
 
 // ---------------------------------------------------------------------------------------------------------- join
-// WPQ warps per (row, query head); each takes every WPQ-th of the query's partial results, a lane finding one at a time.
+// A warp, or WPQ of them, joins QPW neighbouring query heads of a row: they belong to one key-value head and one query tile, so
+// that where their partial results lie is found out once for all of them, which takes longer than adding them up.  A lane finds
+// one partial result at a time; of several warps each takes every WPQ-th.
 constexpr int kMaxWorkers = 2 * kSMs;
 constexpr int kJoinThreads = 128;
 
-template <int DT, int WPQ, int OWN>
+template <int DT, int WPQ, int OWN, int QPW>
 __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_kernel(const __grid_constant__ AttendArgs g) {
     using T = typename PoolIo<DT>::type;
-    constexpr int kJoinWarps = kJoinThreads / 32, kQueries = kJoinWarps / WPQ, kOwn = OWN, kBatch = OWN == 1 ? 8 : 4;
+    constexpr int kJoinWarps = kJoinThreads / 32, kItems = kJoinWarps / WPQ, kOwn = OWN, kBatch = 8 / (OWN * QPW) > 2 ? 8 / (OWN * QPW) : 2;
     __shared__ __align__(16) float acc[WPQ == 1 ? 1 : WPQ][kMaxHeadDim];  // read and written 16 bytes at a time
     __shared__ float2 stats[kJoinWarps];
+    static_assert(WPQ == 1 || QPW == 1, "warps share one query");
     chain_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub_warp = warp % WPQ;
-    const int item = blockIdx.x * kQueries + warp / WPQ;
-    if (item >= g.c.R * g.a.Hq) return;  // the warps of a query agree
-    const int row = div_by(item, g.by_heads), qh = item - row * g.a.Hq;
+    const int item = blockIdx.x * kItems + warp / WPQ, per_row = g.a.Hq / QPW;
+    if (item >= g.c.R * per_row) return;  // the warps of a query agree
+    const int row = div_by(item, g.by_heads), qh = (item - row * per_row) * QPW;
     const int tile = row / kTileRows, in_tile = row % kTileRows, head = div_by(qh, g.by_ratio), sub = qh - head * g.l.ls.ratio;
     const TilePlan& tp = g.l.plans[tile];
     const LineShape& ls = g.l.ls;
@@ -1552,17 +1565,22 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
     const ItemCost full = item_cost<DT>(kTileQueries);
     const int64_t line_at = b.before + head * tp.cost, tile_slots = ((int64_t)tile * ls.H + head) * (kTileRows * kRowSegs * ls.ratio);
 
-    float top = -INFINITY, total = 0.f;
-    float4 o[kOwn];
+    float top[QPW], total[QPW];
+    float4 o[QPW][kOwn];
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) o[i] = float4{0.f, 0.f, 0.f, 0.f};
+    for (int v = 0; v < QPW; ++v) {
+        top[v] = -INFINITY;
+        total[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) o[v][i] = float4{0.f, 0.f, 0.f, 0.f};
+    }
 #pragma unroll 1
     for (int s0 = 0; s0 < n_segs; s0 += 32) {
         if (s0 > 0) {
             seg = *reinterpret_cast<const int4*>(&tp.seg[s0 + lane]);
             seg_start = tp.seg[s0 + lane].start;
         }
-        // a lane per segment: the shares k0 .. k0 + n - 1 that have, or might have, a part of this query's item
+        // a lane per segment: the shares k0 .. k0 + n - 1 that have, or might have, a part of the queries' item
         const uint32_t mask = (uint32_t)seg.x;
         int k0 = 0, n = 0, steps = 0, in_item = 0;
         ItemCost c{1, 0};
@@ -1595,86 +1613,100 @@ __global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_ker
             const int64_t ea = __shfl_sync(kFull, (long long)a, at), efirst = __shfl_sync(kFull, (long long)first, at);
             const ItemCost ec{__shfl_sync(kFull, c.step, at), __shfl_sync(kFull, c.fixed, at)};
             const int esteps = __shfl_sync(kFull, steps, at), ein = __shfl_sync(kFull, in_item, at);
-            int64_t slot = -1;
-            float2 st = float2{-INFINITY, 0.f};
+            int64_t slot = -1;  // of the first of the queries; the others follow
             if (e < all) {
                 const int from = steps_before(k * b.share, ea, ec, esteps);
                 if (from < steps_before((k + 1) * b.share, ea, ec, esteps))  // (a share may lie between two steps)
                     slot = from == 0 ? efirst : g.l.first_rest + (int64_t)k * kTileQueries + ein;
             }
-            if (slot >= 0) st = g.l.stat[slot];
-            // into the running result: the largest reference decides, the others' weights are 2^(their reference - it)
-            const float high = fmaxf(top, warp_max(st.x));
-            const Moved<DT> held(top == high ? 0.f : top - high), to(st.x == high ? 0.f : st.x - high);
-            const float keep = held.factor(), f = to.factor();
-            total = held.sum(total) + warp_sum(to.sum(st.y));
-            top = high;
+            float2 st[QPW];
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i) o[i] = float4{o[i].x * keep, o[i].y * keep, o[i].z * keep, o[i].w * keep};
+            for (int v = 0; v < QPW; ++v) st[v] = slot >= 0 ? g.l.stat[slot + v] : float2{-INFINITY, 0.f};
+            // into the running result: the largest reference decides, the others' weights are 2^(their reference - it)
+            float f[QPW];
+#pragma unroll
+            for (int v = 0; v < QPW; ++v) {
+                const float high = fmaxf(top[v], warp_max(st[v].x));
+                const Moved<DT> held(top[v] == high ? 0.f : top[v] - high), to(st[v].x == high ? 0.f : st[v].x - high);
+                f[v] = to.factor();
+                total[v] = held.sum(total[v]) + warp_sum(to.sum(st[v].y));
+                top[v] = high;
+                const float keep = held.factor();
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) o[v][i] = float4{o[v][i].x * keep, o[v][i].y * keep, o[v][i].z * keep, o[v][i].w * keep};
+            }
             uint32_t have = __ballot_sync(kFull, slot >= 0);
             while (have) {
-                float4 x[kBatch][kOwn];
-                float fu[kBatch];
+                float4 x[kBatch][QPW][kOwn];
+                int from[kBatch];
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    const int from = have ? __ffs(have) - 1 : -1;
+                    from[u] = have ? __ffs(have) - 1 : -1;
                     have &= have - 1;
-                    const int64_t su = __shfl_sync(kFull, (long long)slot, from & 31);
-                    fu[u] = __shfl_sync(kFull, f, from & 31);
-                    if (from < 0) fu[u] = 0.f;
+                    const int64_t su = __shfl_sync(kFull, (long long)slot, from[u] & 31);
 #pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        const int d = lane * 4 + i * 128;
-                        x[u][i] = float4{0.f, 0.f, 0.f, 0.f};
-                        if (from >= 0 && d < g.c.D) x[u][i] = *reinterpret_cast<const float4*>(g.l.part + su * g.c.D + d);
-                    }
+                    for (int v = 0; v < QPW; ++v)
+#pragma unroll
+                        for (int i = 0; i < kOwn; ++i) {
+                            const int d = lane * 4 + i * 128;
+                            x[u][v][i] = float4{0.f, 0.f, 0.f, 0.f};
+                            if (from[u] >= 0 && d < g.c.D) x[u][v][i] = *reinterpret_cast<const float4*>(g.l.part + (su + v) * g.c.D + d);
+                        }
                 }
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u)
 #pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        o[i].x = fmaf(fu[u], x[u][i].x, o[i].x);
-                        o[i].y = fmaf(fu[u], x[u][i].y, o[i].y);
-                        o[i].z = fmaf(fu[u], x[u][i].z, o[i].z);
-                        o[i].w = fmaf(fu[u], x[u][i].w, o[i].w);
+                    for (int v = 0; v < QPW; ++v) {
+                        const float fv = __shfl_sync(kFull, f[v], from[u] & 31);
+                        if (from[u] < 0) continue;
+#pragma unroll
+                        for (int i = 0; i < kOwn; ++i) {
+                            o[v][i].x = fmaf(fv, x[u][v][i].x, o[v][i].x);
+                            o[v][i].y = fmaf(fv, x[u][v][i].y, o[v][i].y);
+                            o[v][i].z = fmaf(fv, x[u][v][i].z, o[v][i].z);
+                            o[v][i].w = fmaf(fv, x[u][v][i].w, o[v][i].w);
+                        }
                     }
             }
         }
     }
     if (WPQ > 1) {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) *reinterpret_cast<float4*>(&acc[sub_warp][lane * 4 + i * 128]) = o[i];
-        if (lane == 0) stats[warp] = float2{top, total};
+        for (int i = 0; i < kOwn; ++i) *reinterpret_cast<float4*>(&acc[sub_warp][lane * 4 + i * 128]) = o[0][i];
+        if (lane == 0) stats[warp] = float2{top[0], total[0]};
         __syncthreads();
         if (sub_warp != 0) return;
-        for (int w = 0; w < WPQ; ++w) top = fmaxf(top, stats[w].x);
-        total = 0.f;
+        for (int w = 0; w < WPQ; ++w) top[0] = fmaxf(top[0], stats[w].x);
+        total[0] = 0.f;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) o[i] = float4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < kOwn; ++i) o[0][i] = float4{0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < WPQ; ++w) {
             const float2 st = stats[w];
-            const Moved<DT> to(st.x == top ? 0.f : st.x - top);
+            const Moved<DT> to(st.x == top[0] ? 0.f : st.x - top[0]);
             const float f = to.factor();
-            total += to.sum(st.y);
+            total[0] += to.sum(st.y);
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
                 const float4 x = *reinterpret_cast<const float4*>(&acc[w][lane * 4 + i * 128]);
-                o[i].x = fmaf(f, x.x, o[i].x);
-                o[i].y = fmaf(f, x.y, o[i].y);
-                o[i].z = fmaf(f, x.z, o[i].z);
-                o[i].w = fmaf(f, x.w, o[i].w);
+                o[0][i].x = fmaf(f, x.x, o[0][i].x);
+                o[0][i].y = fmaf(f, x.y, o[0][i].y);
+                o[0][i].z = fmaf(f, x.z, o[0][i].z);
+                o[0][i].w = fmaf(f, x.w, o[0][i].w);
             }
         }
     }
-    T* out = static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)qh * g.a.out.stride_head;
-    const float inv = total == 0.f ? 0.f : 1.f / total;  // no positions: zeros
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        const int d = lane * 4 + i * 128;
-        if (d >= g.c.D) continue;
-        put4(out + d, float4{o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv});
+    for (int v = 0; v < QPW; ++v) {
+        T* out = static_cast<T*>(g.a.out.data) + (int64_t)row * g.a.out.stride_row + (int64_t)(qh + v) * g.a.out.stride_head;
+        const float inv = total[v] == 0.f ? 0.f : 1.f / total[v];  // no positions: zeros
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int d = lane * 4 + i * 128;
+            if (d >= g.c.D) continue;
+            put4(out + d, float4{o[v][i].x * inv, o[v][i].y * inv, o[v][i].z * inv, o[v][i].w * inv});
+        }
+        if (lane == 0 && g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh + v] = total[v] == 0.f ? -INFINITY : kLn2 * (top[v] + log2f(total[v]));
     }
-    if (lane == 0 && g.a.lse) g.a.lse[(int64_t)row * g.a.Hq + qh] = total == 0.f ? -INFINITY : kLn2 * (top + log2f(total));
 }
 
 // ---------------------------------------------------------------------------------------------------------- launches
@@ -1734,7 +1766,6 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.by_block = fast_div(c.block_len);
     g.l.ls = LineShape{S::kStep, S::kGroup, a.Hq / c.H, c.H};
     g.by_ratio = fast_div(g.l.ls.ratio);
-    g.by_heads = fast_div(a.Hq);
     g.q_words = ((uint64_t)(uintptr_t)a.q.data % 4 == 0 && a.q.stride_row % 2 == 0 && a.q.stride_head % 2 == 0) ? 1 : 0;
     g.q_units = ((uint64_t)(uintptr_t)a.q.data % 16 == 0 && a.q.stride_row % 8 == 0 && a.q.stride_head % 8 == 0 && c.D % 8 == 0) ? 1 : 0;
     TilePlan* plans = reinterpret_cast<TilePlan*>(scratch + sc.plans);
@@ -1770,8 +1801,17 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     // with one warp 106; 896 queries of 32 rows 54 and 52; 16384 of 512 rows 229 and 161)
     const int64_t queries = (int64_t)c.R * a.Hq;
     constexpr int kOwn = DP > 128 ? 2 : 1;
-    if (queries <= 2 * kSMs) return launch_chained(paged_join_kernel<DT, 4, kOwn>, dim3((unsigned)queries), dim3(kJoinThreads), 0, stream, g);
-    return launch_chained(paged_join_kernel<DT, 1, kOwn>, dim3((unsigned)((queries + 3) / 4)), dim3(kJoinThreads), 0, stream, g);
+    const auto join = [&](auto kernel, int per_warp, int per_cta) {
+        g.by_heads = fast_div(a.Hq / per_warp);
+        return launch_chained(kernel, dim3((unsigned)((queries / per_warp + per_cta - 1) / per_cta)), dim3(kJoinThreads), 0, stream, g);
+    };
+    if (queries <= 2 * kSMs) return join(paged_join_kernel<DT, 4, kOwn, 1>, 1, 1);
+    // Several queries per warp where that still fills the GPU with warps, 24 on an SM (16384 queries of 512 rows 160 -> 153 us, 8192
+    // of 256 rows 140 -> 138; but 512 of 16 rows of 4096 positions 40 -> 59).  A query tile is a multiple of 4 queries.
+    const int64_t full = queries / (24 * kSMs);
+    if (kOwn == 1 && full >= 4 && g.l.ls.ratio % 4 == 0) return join(paged_join_kernel<DT, 1, kOwn, 4 / kOwn>, 4 / kOwn, 4);
+    if (full >= 2 && g.l.ls.ratio % 2 == 0) return join(paged_join_kernel<DT, 1, kOwn, 2>, 2, 4);
+    return join(paged_join_kernel<DT, 1, kOwn, 1>, 1, 4);
 }
 
 template <int DT>

@@ -8,6 +8,10 @@
 // Bound by bytes for prompts and by latency for single tokens.  A token has a warp of its own, or several that share its
 // heads while there are too few tokens to fill the GPU; each computes the token's cosines and sines (two or four per lane)
 // for itself, so that warps never wait for each other.
+//
+// Measured (in a graph; 32 or 28 query and 8 or 4 key-value heads of 128): 512 tokens into a bf16 cache 7.7 us (bytes alone 1.9:
+// launch, position, table entry and operands follow one another), 4099 tokens 19 us (11.5), 10,000 tokens into an 8-bit cache
+// 55 us; 4 tokens of 4 fp32 heads 2.9 us.
 #include "paged_common.cuh"
 
 namespace psmc {
@@ -283,7 +287,8 @@ cudaError_t launch(const PagedView& c, PagedWrite w, cudaStream_t stream) {
     using T = typename PoolIo<DT>::type;
     constexpr int kFullVec = 16 / sizeof(T);
     // Elements per access: 16 bytes where every head starts on such a boundary and no access straddles the two halves
-    // (or a pair, or the end) of the rotated part; else two elements (any even rotation of such heads), else one.
+    // (or a pair, or the end) of the rotated part; else two elements (any even rotation of such heads), else one (4099 tokens
+    // 19, 62 and 72 us).
     uint64_t bits = 0;
     for (const HeadsView* h : {&w.in[0], &w.in[1], &w.in[2], &w.q_out})
         if (h->data) bits |= (uint64_t)(uintptr_t)h->data | (uint64_t)(h->stride_row * sizeof(T)) | (uint64_t)(h->stride_head * sizeof(T));
@@ -295,7 +300,8 @@ cudaError_t launch(const PagedView& c, PagedWrite w, cudaStream_t stream) {
     int lph = 1;
     while (lph < 32 && lph * vec < c.D) lph *= 2;
     w.lanes_per_head = lph;
-    // the fewest warps per token that leave none of the GPU's idle (24 resident warps per SM)
+    // the fewest warps per token that leave none of the GPU's idle (24 resident warps per SM): 512 tokens 7.7 us, with one warp
+    // each 9.6; 4 tokens 2.9 and 3.4
     constexpr int kWarps = kWriteThreads / 32;
     w.warps_per_token = 1;
     const int rounds = ((w.q ? w.Hq : 0) + 2 * c.H + 32 / lph - 1) / (32 / lph);

@@ -133,6 +133,10 @@ SHAPES = [  # dt, H, queries per key-value head, D, page, lens, share
     ("f8", 2, 1, 256, 32, [130, 999], 1),
     ("f8", 2, 20, 80, 8, [333, 333, 332], 3),
     ("f8", 1, 4, 112, 16, [4000], 1),
+    # so many query heads that a joining warp takes four or two of them
+    ("bf16", 4, 8, 64, 16, [20 + 3 * (r // 8) for r in range(450)], 8),
+    ("f8", 2, 14, 64, 8, [(37 * (r // 4)) % 300 for r in range(260)], 4),
+    ("bf16", 1, 64, 256, 16, [70 + r // 16 for r in range(112)], 16),
 ]
 
 
