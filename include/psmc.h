@@ -355,8 +355,9 @@ psmc_status psmc_paged_write(const psmc_paged_kv* kv, int n, const int32_t* rows
 /* out[r, h] = sum_p softmax_p(scale * q[r, h] . k_p) v_p over the positions p < lens[r] + extra of row r, for query heads
  * h = 0 .. Hq-1 (a multiple of H: head h reads key-value head h / (Hq / H)).  lse (DEVICE [R, Hq] fp32, may be NULL)
  * receives ln sum_p exp(scale * q . k_p), so that results over parts of a context can be joined.  A row without
- * positions gets zeros and lse = -inf; rows with skip[r] != 0 are left as they were.  Leading blocks that rows of one run of 32 (rows 32 i .. 32 i + 31)
- * share are read once for all of them, unless so few rows of so little room are asked for that it would not pay.  scratch: psmc_paged_attend_scratch_bytes() bytes,
+ * positions gets zeros and lse = -inf; rows with skip[r] != 0 are left as they were.  Leading blocks that rows of one
+ * run of 32 (rows 32 i .. 32 i + 31) share are read once for all of them, unless the rows are so few that every one of
+ * them gets thread blocks of its own.  scratch: psmc_paged_attend_scratch_bytes() bytes,
  * 256-byte aligned, contents irrelevant; calls that may overlap (other streams, graphs replayed side by side) need
  * scratch of their own.  out may not overlap q.  max_blocks * block_len and R * Hq up to 2^27. */
 size_t psmc_paged_attend_scratch_bytes(int R, int n_q_heads, int n_kv_heads, int head_dim);

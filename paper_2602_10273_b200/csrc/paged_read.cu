@@ -1,14 +1,15 @@
 // The paged cache, gathered into dense tensors [R, H, max_len, D] (8-bit codes become the bf16 values they stand for,
 // exactly: a code has 4 significant bits).  Bound by bytes: every live position is read and written once.
 // A CTA takes one block of one row, keys or values: H x live positions x D, 16 bytes of output per lane and access.
-// Measured (in a graph): 32 rows of 4211 positions, 4 heads of 128, bf16, half of the blocks shared by all, 63 us = 4.65 TB/s
-// of distinct bytes (copy rate of this GPU 6.56 TB/s); 8 rows of up to 130 positions, 8-bit, 3.9 us.
+// Measured (in a graph): 32 rows of 4211 positions, 4 heads of 128, bf16, half of the blocks shared by all, 45 us = 6.5 TB/s
+// of distinct bytes (copy rate of this GPU 6.56 TB/s); 8 rows of up to 130 positions, 8-bit, 3.9 us.  128 threads per CTA and
+// stores that leave L2 to the shared blocks: with 256 threads 49 us, with plain stores as well 63; with 64 threads 47.
 #include "paged_common.cuh"
 
 namespace psmc {
 namespace {
 
-constexpr int kReadThreads = 256;
+constexpr int kReadThreads = 128;
 
 template <int DT, int VEC>
 __global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const PagedView c, const PagedRead a, const FastDiv by_access,
@@ -63,7 +64,8 @@ __global__ void __launch_bounds__(kReadThreads) paged_read_kernel(const PagedVie
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) wide[u].x[i] = from_float<T>(code_value(codes[u].x[i]) * s);
             }
-            *reinterpret_cast<Chunk<T, VEC>*>(dst + to[u]) = wide[u];
+            if constexpr (VEC * sizeof(T) == 16) __stcs(reinterpret_cast<uint4*>(dst + to[u]), *reinterpret_cast<const uint4*>(&wide[u]));
+            else *reinterpret_cast<Chunk<T, VEC>*>(dst + to[u]) = wide[u];
         }
     }
 }
@@ -74,7 +76,7 @@ cudaError_t launch(const PagedView& c, const PagedRead& a, cudaStream_t stream) 
     constexpr int kFullVec = 16 / sizeof(T);
     uint64_t bits = (uint64_t)(a.stride_row * sizeof(T)) | (uint64_t)(a.stride_head * sizeof(T)) | (uint64_t)(uintptr_t)a.k |
                     (uint64_t)(uintptr_t)a.v;
-    // 16 bytes per access where every destination row starts on such a boundary, else one element (32 rows 63 and 259 us)
+    // 16 bytes per access where every destination row starts on such a boundary, else one element (32 rows 63 and 259 us, with plain stores)
     const int vec = bits % 16 == 0 && c.D % kFullVec == 0 ? kFullVec : 1;
     auto fn = vec == kFullVec ? paged_read_kernel<DT, kFullVec> : paged_read_kernel<DT, 1>;
     const FastDiv by_access = fast_div(c.D / vec), by_block = fast_div(c.block_len);

@@ -10,8 +10,8 @@
 // for itself, so that warps never wait for each other.
 //
 // Measured (in a graph; 32 or 28 query and 8 or 4 key-value heads of 128): 512 tokens into a bf16 cache 7.7 us (bytes alone 1.9:
-// launch, position, table entry and operands follow one another), 4099 tokens 19 us (11.5), 10,000 tokens into an 8-bit cache
-// 55 us; 4 tokens of 4 fp32 heads 2.9 us.
+// launch, position, table entry and operands follow one another), 4099 tokens 18 us (11.5), 10,000 tokens into an 8-bit cache
+// and read back 71 us (45); 4 tokens of 4 fp32 heads 2.9 us.
 #include "paged_common.cuh"
 
 namespace psmc {
@@ -56,18 +56,29 @@ struct Lane {
     static constexpr int kChunks = kMaxHeadDim / (VEC * 32) > 0 ? kMaxHeadDim / (VEC * 32) : 1;  // accesses per lane and head, at most
     // Heads of a tensor whose loads a warp has under way at once (one at a time, each would wait for memory by itself), and
     // the warps that this leaves registers for: 10,000 tokens of 48 heads into an 8-bit cache take 55 us with four heads and
-    // 24 warps per SM and 61 us with two and 32; 4099 of 36 heads into a bf16 cache take 22 and 19 us.
+    // 24 warps per SM and 61 us with two and 32; 4099 of 36 heads into a bf16 cache take 22 and 19 us (before the streaming
+    // accesses below).
     static constexpr int kBatch = kChunks > 1 ? 1 : (DT == PSMC_F8 ? 4 : 2);
     static constexpr int kCtas = kChunks > 1 ? 2 : (DT == PSMC_F8 ? 3 : 4);
     struct Ahead {       // one batch
         Vec v[kBatch][kChunks];
     };
+    // Operands are read once, and what is written is not read again here: lines that go first when L2 needs room (10,000 tokens
+    // into an 8-bit cache and read back 75 -> 71 us, 4099 tokens 19.0 -> 18.2)
+    static __device__ __forceinline__ void take(Vec& to, const T* from) {
+        if constexpr (sizeof(Vec) == 16) *reinterpret_cast<uint4*>(&to) = __ldcs(reinterpret_cast<const uint4*>(from));
+        else to = *reinterpret_cast<const Vec*>(from);
+    }
+    static __device__ __forceinline__ void put(T* to, const Vec& x) {
+        if constexpr (sizeof(Vec) == 16) __stcs(reinterpret_cast<uint4*>(to), *reinterpret_cast<const uint4*>(&x));
+        else *reinterpret_cast<Vec*>(to) = x;
+    }
     __device__ __forceinline__ void fetch(Ahead& a, int h, int count, int round, const T* x, int64_t x_step) const {
 #pragma unroll
         for (int b = 0; b < kBatch; ++b)
 #pragma unroll
             for (int k = 0; k < kChunks; ++k)
-                if (h + b * round < count && sub + k * lph < n_chunks) a.v[b][k] = *reinterpret_cast<const Vec*>(x + b * x_step + k * lph * VEC);
+                if (h + b * round < count && sub + k * lph < n_chunks) take(a.v[b][k], x + b * x_step + k * lph * VEC);
     }
     int lph, lane, sub, n_chunks, rot, half;
     bool pairs;
@@ -145,7 +156,7 @@ struct Lane {
 #pragma unroll
                             for (int e = 0; e < VEC; ++e) o.x[e] = from_float<T>(y[k][e]);
                         }
-                        *reinterpret_cast<Vec*>(out + k * lph * VEC) = o;
+                        put(out + k * lph * VEC, o);
                     }
                 } else {
                     // as integers, magnitudes sort like the numbers, infinities and NaN above all others
