@@ -29,7 +29,7 @@
 //
 // Measured (in a graph; copy rate of this GPU 6.56 TB/s): one row of 131071 positions, 32 query and 8 key-value heads of 128,
 // bf16, 102 us = 5.3 TB/s, of which the middle kernel 91; 36 rows of 4096 in the one-kernel form 92 us = 6.6 TB/s; 512 rows in
-// groups of 8 that share half, 64 to 1280 positions, 153 us (distinct blocks alone 67: items are short there, and putting one
+// groups of 8 that share half, 64 to 1280 positions, 146 us (distinct blocks alone 67: items are short there, and putting one
 // together costs as much as 1 to 3 steps); 256 rows of 1 to 2303 positions, 8-bit, 138 us = 4.4 TB/s (conversions of codes
 // issue beside the products); 32 rows of 4211 positions of one ancestry, 28 query heads, 8-bit, 49 us (in the one-kernel form,
 // each row reading its blocks from L2).
@@ -1537,12 +1537,13 @@ __global__ void __launch_bounds__(kThreads, S::kCtas) paged_attend_f32_kernel(co
 // ---------------------------------------------------------------------------------------------------------- join
 // A warp, or WPQ of them, joins QPW neighbouring query heads of a row: they belong to one key-value head and one query tile, so
 // that where their partial results lie is found out once for all of them, which takes longer than adding them up.  A lane finds
-// one partial result at a time; of several warps each takes every WPQ-th.
+// one partial result at a time; of several warps each takes every WPQ-th.  Seven CTAs per SM for four heads (72 registers): 512
+// rows 146 us, with six 152, with eight 150.
 constexpr int kMaxWorkers = 2 * kSMs;
 constexpr int kJoinThreads = 128;
 
 template <int DT, int WPQ, int OWN, int QPW>
-__global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? 6 : 4) paged_join_kernel(const __grid_constant__ AttendArgs g) {
+__global__ void __launch_bounds__(kJoinThreads, OWN == 1 ? (QPW == 4 ? 7 : 6) : 4) paged_join_kernel(const __grid_constant__ AttendArgs g) {
     using T = typename PoolIo<DT>::type;
     constexpr int kJoinWarps = kJoinThreads / 32, kItems = kJoinWarps / WPQ, kOwn = OWN, kBatch = 8 / (OWN * QPW) > 2 ? 8 / (OWN * QPW) : 2;
     __shared__ __align__(16) float acc[WPQ == 1 ? 1 : WPQ][kMaxHeadDim];  // read and written 16 bytes at a time
@@ -1806,7 +1807,7 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
         return launch_chained(kernel, dim3((unsigned)((queries / per_warp + per_cta - 1) / per_cta)), dim3(kJoinThreads), 0, stream, g);
     };
     if (queries <= 2 * kSMs) return join(paged_join_kernel<DT, 4, kOwn, 1>, 1, 1);
-    // Several queries per warp where that still fills the GPU with warps, 24 on an SM (16384 queries of 512 rows 160 -> 153 us, 8192
+    // Several queries per warp where that still fills the GPU with warps, 24 on an SM (16384 queries of 512 rows 160 -> 146 us, 8192
     // of 256 rows 140 -> 138; but 512 of 16 rows of 4096 positions 40 -> 59).  A query tile is a multiple of 4 queries.
     const int64_t full = queries / (24 * kSMs);
     if (kOwn == 1 && full >= 4 && g.l.ls.ratio % 4 == 0) return join(paged_join_kernel<DT, 1, kOwn, 4 / kOwn>, 4 / kOwn, 4);
