@@ -23,7 +23,6 @@ STATIC_SCRATCH_BYTES = 4 << 20
 F32, BF16, F8 = 0, 1, 2
 ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "yarn": 4}
 ROPE_LAYOUTS = {"half": 0, "pairs": 1}
-MAX_HEAD_DIM = 256
 SYSTEMATIC, STRATIFIED, MULTINOMIAL, RESIDUAL = 0, 1, 2, 3
 
 _lib = None
@@ -374,6 +373,7 @@ class Psmc:
         va = (C.c_void_p * n)(*[t.data_ptr() for t in v_pools])
         d = KvPools(n, C.cast(ka, C.POINTER(C.c_void_p)), C.cast(va, C.POINTER(C.c_void_p)), H, D, _dtype_code(p0))
         d._keep = (ka, va, list(k_pools), list(v_pools))
+        d.index = k_pools[0].get_device()
         return d
 
     def make_kv_pools_f8(self, k_pools, v_pools, n_kv_heads: int, head_dim: int):
@@ -386,6 +386,7 @@ class Psmc:
         va = (C.c_void_p * n)(*[t.data_ptr() for t in v_pools])
         d = KvPools(n, C.cast(ka, C.POINTER(C.c_void_p)), C.cast(va, C.POINTER(C.c_void_p)), n_kv_heads, head_dim, F8)
         d._keep = (ka, va, list(k_pools), list(v_pools))
+        d.index = k_pools[0].get_device()
         return d
 
     # ---- a language model's operators on the context's paged cache
@@ -394,12 +395,13 @@ class Psmc:
                        positions: torch.Tensor = None, stream=None):
         """psmc_kv_paged_write: the next token of every live row (k, v [R, H, D], q [R, Hq, D]), or with rows and positions
         (int32 [n]) any tokens.  Returns q_out (q with its rotary positions), allocated if not given."""
-        n, dev = k.shape[0], k.get_device()
+        n, dev = k.shape[0], pools.index
         if rows is None:
             assert positions is None and n == self.R
         else:
             _check_ints(rows, n, dev)
             _check_ints(positions, n, dev)
+        assert rope is None or rope.index == dev
         q_out, Hq = _write_heads(k, v, q, q_out, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, stream)
         at = _heads.at
         _launch(dev, lib().psmc_kv_paged_write, self._h, C.byref(pools), layer, n, _ptr(rows), _ptr(positions), _ref(rope), at, at + 24,
@@ -410,7 +412,7 @@ class Psmc:
                         lse: torch.Tensor = None, scratch: torch.Tensor = None, stream=None):
         """psmc_kv_paged_attend: q [R, Hq, D] of every row's new token over its len + 1 positions (finished rows of out and
         lse are left as they were; zeros in an out allocated here)."""
-        dev = q.get_device()
+        dev = pools.index
         need = lib().psmc_paged_attend_scratch_bytes(self.R, q.shape[1], pools.n_kv_heads, pools.head_dim)
         scratch = _scratch(scratch, need, dev, stream)
         out = _attend_heads(q, out, lse, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev, True, stream)
@@ -421,8 +423,7 @@ class Psmc:
 
     def kv_paged_read(self, pools: KvPools, layer: int, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
         """psmc_kv_paged_read: the live positions of every row into dense [R, H, max_len, D] tensors."""
-        d = k_out if k_out is not None else v_out
-        dev = d.get_device()
+        d, dev = k_out if k_out is not None else v_out, pools.index
         _check_dense(k_out, v_out, d, self.R, pools.n_kv_heads, pools.head_dim, _io_dtype(pools.dt), dev)
         _launch(dev, lib().psmc_kv_paged_read, self._h, C.byref(pools), layer, _ptr(k_out), _ptr(v_out), d.shape[2], d.stride(0),
                 d.stride(1), _raw_stream(stream, dev))
@@ -531,7 +532,7 @@ class Rope(RopeDesc):
     def __init__(self, freqs: torch.Tensor, layout: str = "half", mscale: float = 1.0):
         assert freqs.is_cuda and freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous()
         super().__init__(freqs.data_ptr(), 2 * freqs.numel(), ROPE_LAYOUTS[layout], mscale)
-        self._keep = freqs
+        self._keep, self.index = freqs, freqs.get_device()
 
 
 class PagedKv(PagedKvDesc):
@@ -682,6 +683,7 @@ def paged_write(cache: PagedKv, k: torch.Tensor, v: torch.Tensor, rows, position
     _check_ints(positions, n, dev)
     if skip is not None or status_word is not None:
         _check_optional(skip, status_word, cache.rows, dev)
+    assert rope is None or rope.index == dev
     q_out, Hq = _write_heads(k, v, q, q_out, cache.heads, cache.dim, cache.io, dev, stream)
     at = _heads.at
     _launch(dev, lib().psmc_paged_write, cache.address, n, 0 if rows is None else rows.data_ptr(), positions.data_ptr(),
