@@ -1776,16 +1776,19 @@ cudaError_t launch(const PagedView& c, const PagedAttend& a, cudaStream_t stream
     g.l.first_rest = sc.first_rest;
     g.l.n_tiles = sc.n_tiles;
     g.l.workers = S::kCtas * kSMs;
-    // One CTA per (row, key-value head, query tile), all resident at once, and nothing else: no plan, no join, no cutting.  What
-    // that leaves idle (the CTAs that there is no such item for, over the steps that the table has room for) may be worth 20
+    // One CTA per (row, key-value head, query tile) and nothing else: no plan, no join, no cutting.  Where all are resident at
+    // once, what that leaves idle (the CTAs that there is no such item for, over the steps that the table has room for) may be worth 20
     // steps of the whole GPU, which is what the rest costs: 4 fp32 rows of 121 positions 17 -> 6 us, 8 bf16 rows of 1000
     // positions with 32 heads each 24 -> 16, 16 of 2048 with 8 heads 44 -> 29, 36 of 4096 with 8 heads 115 -> 92; and beyond it
     // 4 of 2048 22 -> 26, 8 8-bit rows of 4096 with 4 heads 25 -> 39.  Blocks that rows share come from L2 then (32 rows of 2048
     // positions, 9 of 10 blocks shared: 45 -> 29 us).  64 steps at most: which rows are short only the device knows, and a
-    // single long one would take a CTA that time.
+    // single long one would take a CTA that time.  Where they are not, up to four times as many over 32 steps at most: 128 bf16
+    // rows of 256, 512 and 1024 positions with 8 heads 45 -> 35, 67 -> 52, 106 -> 87 us, the latter with 4 of 5 blocks shared
+    // 72 -> 66; but 512 such rows of 64 positions 58 -> 71.
     const int64_t direct = (int64_t)c.R * c.H * ((g.l.ls.ratio + kGroups * S::kGroup - 1) / (kGroups * S::kGroup));
     const int64_t room = (int64_t)c.max_blocks * c.block_len, idle = g.l.workers - direct;
-    g.l.direct = idle >= 0 && room <= 64 * S::kStep && room * idle <= (int64_t)20 * S::kStep * g.l.workers ? 1 : 0;
+    const bool resident = idle >= 0 && room <= 64 * S::kStep && room * idle <= (int64_t)20 * S::kStep * g.l.workers;
+    g.l.direct = resident || (idle < 0 && direct <= 4 * g.l.workers && room <= 32 * S::kStep) ? 1 : 0;
     if (g.l.direct) g.l.workers = (int)direct;
     cudaError_t e = g.l.direct ? cudaSuccess : launch_chained(paged_plan_kernel<DT>, dim3((unsigned)sc.n_tiles), dim3(kPlanThreads), 0, stream, c, a, g.l.ls, plans);
     if (e != cudaSuccess) return e;
